@@ -1,0 +1,238 @@
+// New keys and values into the pages of the 4-bit cache, and the boxes of their pages.
+//
+// The tokens of one page form a run of the list: slots that ascend by one and do not cross a
+// page.  One wavefront has one run of one head, so nobody else touches the page's box or shares a
+// byte: the box needs no atomics and does not depend on any order.  A lane has eight channels of four
+// consecutive tokens (16-byte loads); four lanes share a scale.  Bound by memory: 4 D bytes read
+// and 68 D / 64 written per token and head, plus 4 D if the rounded rows are wanted.
+
+#include "kv_internal.h"
+
+namespace ivfpq {
+
+namespace {
+
+// max over the four lanes that share 32 channels (they are aligned to four)
+__device__ inline float quad_max(float x) {
+  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true)));
+  return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x4E, 0xf, 0xf, true)));
+}
+
+// the value of the lane two further within its four
+__device__ inline uint32_t quad_across(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true);
+}
+
+// eight values as codes, the first channel lowest; b: the scale byte of the 32 channels
+template <int DT>
+__device__ inline uint32_t round_row(u32x4 raw, bool bad, uint32_t &b) {
+  float x[8], top = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    x[j] = KvType<DT>::to_float((uint16_t)(raw[j >> 1] >> (16 * (j & 1))));
+    if (bad) x[j] = 0.0f;
+    top = fmaxf(top, fabsf(x[j]));
+  }
+  top = quad_max(top);
+  int e = (int)(__float_as_uint(top) >> 23) - 2;
+  e = e < 1 ? 1 : e > 254 ? 254 : e;
+  b = (uint32_t)e;
+  const float scale = __uint_as_float(b << 23);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+  return w;
+}
+
+template <int DT>
+__device__ inline u32x4 held_row(uint32_t w, uint32_t b) {
+  const float scale = __uint_as_float(b << 23);
+  u32x4 r;
+  r[0] = KvType<DT>::template unpack<0>(w, scale);
+  r[1] = KvType<DT>::template unpack<1>(w, scale);
+  r[2] = KvType<DT>::template unpack<2>(w, scale);
+  r[3] = KvType<DT>::template unpack<3>(w, scale);
+  return r;
+}
+
+template <int DT>
+__device__ inline bool row_bad(u32x4 raw) {
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    bad = bad || KvType<DT>::not_finite((uint16_t)raw[j]) || KvType<DT>::not_finite((uint16_t)(raw[j] >> 16));
+  return bad;
+}
+
+template <int D, int DT>
+__global__ __launch_bounds__(64) void kv_append_kernel(KvAppendArgs a) {
+  constexpr int OCT = D / 8;          // lanes of a token
+  constexpr int QUADS = 64 / OCT;     // groups of four tokens at a time
+  constexpr int STEP = 4 * QUADS;
+  __shared__ float box[2][8][64];
+  const int lane = threadIdx.x;
+  const int h = blockIdx.y;
+  const int64_t i = blockIdx.x;       // token of the list
+  const int64_t slot0 = a.slots[i];
+  if (slot0 < 0 || slot0 >= a.n_slots) return;
+  const int place0 = (int)(slot0 % KV_PAGE);
+  if (place0 != 0 && i > 0 && a.slots[i - 1] == slot0 - 1) return;  // not the first of its run
+  // length of the run: a lane looks at each further place of the page
+  const bool on = lane < KV_PAGE - place0 && i + lane < a.tokens && a.slots[i + lane] == slot0 + lane;
+  const uint64_t miss = ~__ballot(on);
+  const int n = miss ? __builtin_ctzll(miss) : 64;
+
+  const int quad = lane / OCT, oct = lane % OCT;
+  const bool active = lane < QUADS * OCT;
+  const int group = oct >> 2;  // of 32 channels
+  const uint64_t token_mask = (OCT == 64 ? ~0ull : ((1ull << OCT) - 1)) << (active ? quad * OCT : 0);
+  const int64_t page = slot0 / KV_PAGE;
+  char *at = a.pages + (page * a.kv_heads + h) * (int64_t)kv_head_bytes(D);
+  const uint16_t *kp = a.k + h * a.k_head + oct * 8, *vp = a.v + h * a.v_head + oct * 8;
+
+  float low[8], high[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) low[j] = __builtin_inff(), high[j] = -__builtin_inff();
+
+  // groups of four places, from the one that holds the first token
+  for (int g0 = place0 & ~3; g0 < place0 + n; g0 += STEP) {
+    const int t0 = g0 + quad * 4;  // place of the lane's first token
+    u32x4 kr[4], vr[4];
+    bool in[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int place = t0 + j;
+      in[j] = active && place >= place0 && place < place0 + n;
+      kr[j] = u32x4{0, 0, 0, 0};
+      vr[j] = u32x4{0, 0, 0, 0};
+      if (in[j]) {
+        const int64_t row = i + place - place0;
+        kr[j] = *reinterpret_cast<const u32x4 *>(kp + row * a.k_token);
+        vr[j] = *reinterpret_cast<const u32x4 *>(vp + row * a.v_token);
+      }
+    }
+    uint32_t kc[4], vc[4], ks[4], vs[4];
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool bad = (__ballot(row_bad<DT>(kr[j]) || row_bad<DT>(vr[j])) & token_mask) != 0;
+      kc[j] = round_row<DT>(kr[j], bad, ks[j]);
+      vc[j] = round_row<DT>(vr[j], bad, vs[j]);
+      if (in[j]) {
+        any = true;
+        const int place = t0 + j;
+        const u32x4 kh = held_row<DT>(kc[j], ks[j]);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const float x = KvType<DT>::to_float((uint16_t)(kh[c >> 1] >> (16 * (c & 1))));
+          low[c] = fminf(low[c], x);
+          high[c] = fmaxf(high[c], x);
+        }
+        *reinterpret_cast<uint32_t *>(at + place * (D / 2) + oct * 4) = kc[j];
+        if ((oct & 3) == 0)
+          at[kv_kscale_at(D) + ((place % 16) * (D / 32) + group) * 4 + place / 16] = (char)(bad ? 255 : ks[j]);
+        if (a.k_rounded) {
+          const int64_t row = ((i + place - place0) * a.kv_heads + h) * D + oct * 8;
+          const u32x4 nan = u32x4{0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
+          *reinterpret_cast<u32x4 *>(a.k_rounded + row) = bad ? nan : kh;
+        }
+        if (a.v_rounded) {
+          const int64_t row = ((i + place - place0) * a.kv_heads + h) * D + oct * 8;
+          *reinterpret_cast<u32x4 *>(a.v_rounded + row) = held_row<DT>(vc[j], vs[j]);
+        }
+      }
+    }
+    // values: a byte has channels c and c + 16 of one token; the lane two further has the other
+    // nibbles, and each of the two writes four of the eight bytes
+    const bool upper = (oct & 2) != 0;  // this lane's channels are the high nibbles
+    uint32_t bytes[4];                  // byte c: this lane's c-th of the four, per token
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t other = quad_across(vc[j]);
+      const uint32_t lo = upper ? other : vc[j], hi = upper ? vc[j] : other;
+      // channels 0-3 of the octet for the lower lane, 4-7 for the upper one
+      const uint32_t l = (upper ? lo >> 16 : lo) & 0xffff, u = (upper ? hi >> 16 : hi) & 0xffff;
+      uint32_t w = 0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) w |= (((l >> (4 * c)) & 15) | (((u >> (4 * c)) & 15) << 4)) << (8 * c);
+      bytes[j] = w;
+    }
+    if (any) {
+      const bool whole = in[0] && in[1] && in[2] && in[3];
+      char *base = at + kv_v_at(D) + group * 1024 + ((t0 / 4) % 4) * 256 + (t0 / 16) * 4;
+      const int c16 = (oct & 1) * 8 + (upper ? 4 : 0);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        char *to = base + (c16 + c) * 16;
+        if (whole) {
+          *reinterpret_cast<uint32_t *>(to) = ((bytes[0] >> (8 * c)) & 255) | (((bytes[1] >> (8 * c)) & 255) << 8) |
+                                              (((bytes[2] >> (8 * c)) & 255) << 16) | (((bytes[3] >> (8 * c)) & 255) << 24);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (in[j]) to[j] = (char)(bytes[j] >> (8 * c));
+        }
+      }
+      if ((oct & 3) == 0) {
+        char *to = at + kv_vscale_at(D) + group * 64 + ((t0 / 4) % 4) * 16 + (t0 / 16) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (in[j]) to[j] = (char)vs[j];
+      }
+    }
+  }
+
+  // the run's box, joined with what the page's earlier tokens left
+#pragma unroll
+  for (int j = 0; j < 8; ++j) box[0][j][lane] = low[j], box[1][j][lane] = high[j];
+  __syncthreads();
+  if (lane < OCT) {
+    uint16_t *to = a.boxes + ((page * a.kv_heads + h) * 2) * (int64_t)D + oct * 8;
+    u32x4 old[2];
+    if (place0 != 0) {
+      old[0] = *reinterpret_cast<const u32x4 *>(to);
+      old[1] = *reinterpret_cast<const u32x4 *>(to + D);
+    }
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      u32x4 r;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float x = box[side][j][lane];
+#pragma unroll
+        for (int q = 1; q < QUADS; ++q) x = side ? fmaxf(x, box[side][j][lane + q * OCT]) : fminf(x, box[side][j][lane + q * OCT]);
+        if (place0 != 0) {
+          const float was = __uint_as_float((old[side][j >> 1] >> (16 * (j & 1))) << 16);
+          x = side ? fmaxf(x, was) : fminf(x, was);
+        }
+        const uint32_t half = __float_as_uint(x) >> 16;  // exact: two significant bits
+        r[j >> 1] = (j & 1) ? r[j >> 1] | (half << 16) : half;
+      }
+      *reinterpret_cast<u32x4 *>(to + side * D) = r;
+    }
+  }
+}
+
+}  // namespace
+
+template <int D>
+static void append_of(const KvAppendArgs &a, int dtype, hipStream_t s) {
+  const dim3 grid((unsigned)a.tokens, (unsigned)a.kv_heads);
+  if (dtype == IVFPQ_KV_BF16) hipLaunchKernelGGL((kv_append_kernel<D, IVFPQ_KV_BF16>), grid, dim3(64), 0, s, a);
+  else hipLaunchKernelGGL((kv_append_kernel<D, IVFPQ_KV_FP16>), grid, dim3(64), 0, s, a);
+}
+
+int launch_kv_append(const KvAppendArgs &a, int D, int dtype, hipStream_t s) {
+  switch (D) {
+    case 64: append_of<64>(a, dtype, s); break;
+    case 96: append_of<96>(a, dtype, s); break;
+    case 128: append_of<128>(a, dtype, s); break;
+    default: append_of<256>(a, dtype, s); break;
+  }
+  KV_HIP_TRY(hipGetLastError());
+  return IVFPQ_OK;
+}
+
+}  // namespace ivfpq

@@ -1,0 +1,136 @@
+// Shared by the kv_*.hip files: launch arguments and the page's layout (include/ivfpq_kv.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ivfpq_kv.h"
+
+namespace ivfpq {
+
+void set_error(const char *fmt, ...);
+int hip_fail(hipError_t e, const char *what);
+
+constexpr int KV_PAGE = IVFPQ_KV_PAGE;
+// byte offsets within a page and head
+constexpr int kv_kscale_at(int D) { return 32 * D; }
+constexpr int kv_v_at(int D) { return 34 * D; }
+constexpr int kv_vscale_at(int D) { return 66 * D; }
+constexpr int kv_head_bytes(int D) { return 68 * D; }
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+struct KvPlanArgs {
+  const int32_t *past, *fresh;
+  int32_t *table, *free_pages, *kv_lens, *q_start, *token_req, *positions;
+  int64_t *slots;
+  const int64_t *state;
+  int64_t *state_out, capacity;
+  int32_t requests, width, max_tokens, per_group, parts;
+};
+
+struct KvAppendArgs {
+  char *pages;
+  uint16_t *boxes;
+  const uint16_t *k, *v;
+  uint16_t *k_rounded, *v_rounded;
+  const int64_t *slots;
+  int64_t k_token, k_head, v_token, v_head, n_slots, tokens;
+  int32_t kv_heads;
+};
+
+struct KvSelectArgs {
+  const uint16_t *boxes, *q;
+  const int32_t *table, *q_start, *kv_lens, *token_req, *positions;
+  float *scores;  // [tokens][kv_heads][score_width]
+  int32_t *out;
+  int64_t q_token, q_head, n_pages;
+  int32_t kv_heads, group, requests, tokens, width, score_width, n_select, sinks, recent;
+};
+
+struct KvAttnArgs {
+  const char *pages;
+  const uint16_t *q;
+  uint16_t *out;
+  float *lse;
+  const int32_t *table, *q_start, *kv_lens, *token_req, *positions, *selected;
+  int64_t q_token, q_head, out_token, out_head, n_pages;
+  int32_t kv_heads, group, requests, tokens, width, n_select, window;
+  float scale2;  // scale * log2(e)
+  // split over pages: workgroup w takes [w, w + 1) * span of the (group, head, tile, page) units in order
+  int32_t n_wg, scanned;
+  int64_t *prefix;  // [groups + 1]: units before a group, then the span (written by the scan, read by the join)
+  float *part_ml;   // [2 n_wg][rows][2]
+  float *part_o;    // [2 n_wg][rows][D]
+};
+
+int launch_kv_plan(const KvPlanArgs &a, hipStream_t s);
+int launch_kv_append(const KvAppendArgs &a, int D, int dtype, hipStream_t s);
+int launch_kv_select(const KvSelectArgs &a, int D, int dtype, hipStream_t s);
+size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int n_select,
+                              int64_t width);
+int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s);
+
+#define KV_HIP_TRY(expr)                                \
+  do {                                                  \
+    hipError_t _e = (expr);                             \
+    if (_e != hipSuccess) return hip_fail(_e, #expr);   \
+  } while (0)
+
+// Element types: the conversions and products of bf16 and fp16 rows.
+template <int DTYPE>
+struct KvType;
+
+template <>
+struct KvType<IVFPQ_KV_BF16> {
+  typedef __bf16 elem;
+  typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+  static __device__ inline float to_float(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
+  static __device__ inline bool not_finite(uint16_t u) { return (u & 0x7f80) == 0x7f80; }
+  static __device__ inline uint32_t pack(float a, float b) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const f2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, x2));
+  }
+  // two held values from byte SEL of w: the low nibble in the low half
+  template <int SEL>
+  static __device__ inline uint32_t unpack(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
+  }
+  static __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+};
+
+template <>
+struct KvType<IVFPQ_KV_FP16> {
+  typedef _Float16 elem;
+  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+  static __device__ inline float to_float(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
+  static __device__ inline bool not_finite(uint16_t u) { return (u & 0x7c00) == 0x7c00; }
+  static __device__ inline uint32_t pack(float a, float b) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const f2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, x2));
+  }
+  template <int SEL>
+  static __device__ inline uint32_t unpack(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, SEL));
+  }
+  static __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+};
+
+// 2^(b - 127) of byte I of w, b >= 1
+template <int I>
+__device__ inline float kv_scale(uint32_t w) {
+  return __uint_as_float(I == 3 ? (w >> 1) & 0x7f800000u : ((w >> (8 * I)) & 0xffu) << 23);
+}
+
+}  // namespace ivfpq

@@ -1,0 +1,168 @@
+// Page tables and slot maps of a step from the requests' lengths, on the device: a server that
+// builds them on the host has to bring the lengths back first.
+//
+// One launch.  Workgroup (b, part) owns per_group requests; it sums what all requests before them
+// add, take and give back (8 bytes a request, from L2), scans its own, and writes their part of
+// the slots, the table and the ring.  Nothing is written that another workgroup reads: the new
+// counters go to an array of their own, pages are taken from [head, tail) of the ring and given
+// back behind tail, entries of the table are read below ceil(past / 64) and written from there.
+
+#include "kv_internal.h"
+
+namespace ivfpq {
+
+namespace {
+
+struct Counts {
+  int32_t past, fresh, held, take, give;
+};
+
+// a request's lengths, cut to what its row of the table has room for
+__device__ inline Counts counts_of(int32_t past, int32_t fresh, int32_t width) {
+  Counts c;
+  const int64_t room = (int64_t)width * KV_PAGE;
+  c.past = past < 0 ? 0 : (int32_t)(past < room ? past : room);
+  c.fresh = fresh < 0 ? 0 : fresh;
+  c.held = (int32_t)(((int64_t)c.past + KV_PAGE - 1) / KV_PAGE);
+  int64_t total = (int64_t)c.past + c.fresh;
+  total = total < room ? total : room;
+  c.take = fresh < 0 ? 0 : (int32_t)((total + KV_PAGE - 1) / KV_PAGE) - c.held;
+  c.give = fresh < 0 ? c.held : 0;
+  return c;
+}
+
+__device__ inline int64_t wave_sum(int64_t v) {
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+constexpr int PLAN_PER_GROUP = 64;  // most requests that a workgroup owns
+
+__global__ __launch_bounds__(256) void kv_plan_kernel(KvPlanArgs a) {
+  __shared__ int64_t before[3], sums[4][3];
+  __shared__ int32_t own[PLAN_PER_GROUP][5];  // first token, first page taken, first page given, past, fresh
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r0 = blockIdx.x * a.per_group, part = blockIdx.y;
+  const int n_own = min(a.per_group, a.requests - r0);
+
+  int64_t s0 = 0, s1 = 0, s2 = 0;
+#pragma unroll 4
+  for (int r = tid; r < r0; r += 256) {
+    const Counts c = counts_of(a.past[r], a.fresh[r], a.width);
+    s0 += c.fresh;
+    s1 += c.take;
+    s2 += c.give;
+  }
+  s0 = wave_sum(s0);
+  s1 = wave_sum(s1);
+  s2 = wave_sum(s2);
+  if (lane == 0) sums[wave][0] = s0, sums[wave][1] = s1, sums[wave][2] = s2;
+  __syncthreads();
+  if (wave == 0) {
+    // own requests, a lane each, scanned behind the sums
+    Counts c = {0, 0, 0, 0, 0};
+    int32_t fresh_raw = 0;
+    if (lane < n_own) {
+      fresh_raw = a.fresh[r0 + lane];
+      c = counts_of(a.past[r0 + lane], fresh_raw, a.width);
+    }
+    int64_t t0 = c.fresh, t1 = c.take, t2 = c.give;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t u0 = __shfl_up(t0, d), u1 = __shfl_up(t1, d), u2 = __shfl_up(t2, d);
+      if (lane >= d) t0 += u0, t1 += u1, t2 += u2;
+    }
+    for (int w = 0; w < 4; ++w) t0 += sums[w][0], t1 += sums[w][1], t2 += sums[w][2];
+    if (lane < n_own) {
+      own[lane][0] = (int32_t)min(t0 - c.fresh, (int64_t)a.max_tokens);
+      own[lane][1] = (int32_t)min(t1 - c.take, (int64_t)0x7fffffff);
+      own[lane][2] = (int32_t)min(t2 - c.give, (int64_t)0x7fffffff);
+      own[lane][3] = c.past;
+      own[lane][4] = fresh_raw;
+      if (part == 0) {
+        const int64_t room = (int64_t)a.width * KV_PAGE, total = (int64_t)c.past + c.fresh;
+        a.kv_lens[r0 + lane] = fresh_raw < 0 ? 0 : (int32_t)(total < room ? total : room);
+        a.q_start[r0 + lane] = own[lane][0];
+      }
+    }
+    if (lane == 63) before[0] = t0, before[1] = t1, before[2] = t2;
+  }
+  __syncthreads();
+
+  const int64_t head = a.state[0], tail = a.state[1];
+  const int64_t avail = tail > head ? min(tail - head, a.capacity) : 0;
+  const int32_t cap = (int32_t)a.capacity;
+  int32_t head_at = (int32_t)(head % a.capacity), tail_at = (int32_t)(tail % a.capacity);
+  if (head_at < 0) head_at += cap;  // counters that were never set up: still inside the ring
+  if (tail_at < 0) tail_at += cap;
+  const bool last = r0 + n_own == a.requests;
+  if (last && part == 0 && tid == 0) {
+    const int64_t used = min(before[1], avail);
+    a.state_out[0] = head + used;
+    a.state_out[1] = tail + before[2];
+    a.state_out[2] = before[1] - used;
+    a.q_start[a.requests] = (int32_t)min(before[0], (int64_t)a.max_tokens);
+  }
+
+  const int n_waves = 4 * a.parts, w = part * 4 + wave;  // all of them on one request after the other when there are few
+  for (int i = a.parts == 1 ? wave : 0; i < n_own; i += a.parts == 1 ? 4 : 1) {
+    const int r = r0 + i, first = a.parts == 1 ? lane : w * 64 + lane, stride = a.parts == 1 ? 64 : n_waves * 64;
+    const int32_t past = own[i][3], fresh = own[i][4];
+    const Counts c = counts_of(past, fresh, a.width);
+    int32_t *row = a.table + (int64_t)r * a.width;
+    // page `take` of this request, or -1
+    auto taken = [&](int32_t j) -> int32_t {
+      const int64_t n = (int64_t)own[i][1] + j;
+      if (n >= avail) return -1;
+      int64_t at = head_at + n;
+      if (at >= cap) at -= cap;
+      return a.free_pages[at];
+    };
+    for (int j = first; j < c.give; j += stride) {
+      const int64_t n = (int64_t)own[i][2] + j;
+      if (n < a.capacity) {
+        int64_t at = tail_at + n;
+        if (at >= cap) at -= cap;
+        a.free_pages[at] = row[j];
+      }
+    }
+    for (int j = first; j < c.take; j += stride) row[c.held + j] = taken(j);
+    for (int64_t j = first; j < c.fresh; j += stride) {
+      const int64_t t = own[i][0] + j, pos = c.past + j;
+      if (t >= a.max_tokens) break;
+      const int64_t col = pos / KV_PAGE;
+      int32_t page = -1;
+      if (col < c.held) page = row[col];
+      else if (col < c.held + c.take) page = taken((int32_t)(col - c.held));
+      a.slots[t] = page >= 0 ? (int64_t)page * KV_PAGE + pos % KV_PAGE : -1;
+      a.token_req[t] = r;
+      a.positions[t] = (int32_t)pos;
+    }
+  }
+  if (last)  // rows that stand for no token
+    for (int64_t t = before[0] + part * 256 + tid; t < a.max_tokens; t += (int64_t)a.parts * 256) {
+      a.slots[t] = -1;
+      a.token_req[t] = -1;
+      a.positions[t] = -1;
+    }
+}
+
+}  // namespace
+
+int launch_kv_plan(const KvPlanArgs &args, hipStream_t s) {
+  KvPlanArgs a = args;
+  // a wavefront for each request when there are many; all of a part's wavefronts on one request
+  // after the other when there are few and each may have many tokens
+  a.per_group = a.requests >= 64 ? 16 : 1;
+  const int64_t groups = a.requests > 0 ? (a.requests + a.per_group - 1) / a.per_group : 1;
+  int64_t parts = 1;
+  if (a.requests < 64) {
+    const int64_t want = ((int64_t)a.max_tokens + 1023) / 1024, most = 512 / groups;
+    parts = want < 1 ? 1 : want > most ? most : want;
+  }
+  a.parts = (int32_t)parts;
+  hipLaunchKernelGGL(kv_plan_kernel, dim3((unsigned)groups, (unsigned)parts), dim3(256), 0, s, a);
+  KV_HIP_TRY(hipGetLastError());
+  return IVFPQ_OK;
+}
+
+}  // namespace ivfpq
