@@ -1,7 +1,7 @@
 // New keys and values into the pages of the 4-bit cache, and the boxes of their pages.
 //
 // The tokens of one page form a run of the list: slots that ascend by one and do not cross a
-// page.  One wavefront has one run of one head, so nobody else touches the page's box or shares a
+// page.  One workgroup has one run of one head, so nobody else touches the page's box or shares a
 // byte: the box needs no atomics and does not depend on any order.  A lane has eight channels of four
 // consecutive tokens (16-byte loads); four lanes share a scale.  Bound by memory: 4 D bytes read
 // and 68 D / 64 written per token and head, plus 4 D if the rounded rows are wanted.
@@ -66,24 +66,14 @@ __device__ inline bool row_bad(u32x4 raw) {
   return bad;
 }
 
+// A run's tokens whose places p have (p / STEP) % of == turn: codes, scales, rounded rows; the lane's eight channels' box.
 template <int D, int DT>
-__global__ __launch_bounds__(64) void kv_append_kernel(KvAppendArgs a) {
+__device__ inline void write_run(const KvAppendArgs &a, int64_t i, int64_t slot0, int n, int h, int lane, int turn, int of,
+                                 float *low, float *high) {
   constexpr int OCT = D / 8;          // lanes of a token
   constexpr int QUADS = 64 / OCT;     // groups of four tokens at a time
   constexpr int STEP = 4 * QUADS;
-  __shared__ float box[2][8][64];
-  const int lane = threadIdx.x;
-  const int h = blockIdx.y;
-  const int64_t i = blockIdx.x;       // token of the list
-  const int64_t slot0 = a.slots[i];
-  if (slot0 < 0 || slot0 >= a.n_slots) return;
   const int place0 = (int)(slot0 % KV_PAGE);
-  if (place0 != 0 && i > 0 && a.slots[i - 1] == slot0 - 1) return;  // not the first of its run
-  // length of the run: a lane looks at each further place of the page
-  const bool on = lane < KV_PAGE - place0 && i + lane < a.tokens && a.slots[i + lane] == slot0 + lane;
-  const uint64_t miss = ~__ballot(on);
-  const int n = miss ? __builtin_ctzll(miss) : 64;
-
   const int quad = lane / OCT, oct = lane % OCT;
   const bool active = lane < QUADS * OCT;
   const int group = oct >> 2;  // of 32 channels
@@ -92,12 +82,11 @@ __global__ __launch_bounds__(64) void kv_append_kernel(KvAppendArgs a) {
   char *at = a.pages + (page * a.kv_heads + h) * (int64_t)kv_head_bytes(D);
   const uint16_t *kp = a.k + h * a.k_head + oct * 8, *vp = a.v + h * a.v_head + oct * 8;
 
-  float low[8], high[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) low[j] = __builtin_inff(), high[j] = -__builtin_inff();
 
   // groups of four places, from the one that holds the first token
-  for (int g0 = place0 & ~3; g0 < place0 + n; g0 += STEP) {
+  for (int g0 = (place0 & ~3) + turn * STEP; g0 < place0 + n; g0 += of * STEP) {
     const int t0 = g0 + quad * 4;  // place of the lane's first token
     u32x4 kr[4], vr[4];
     bool in[4];
@@ -184,33 +173,83 @@ __global__ __launch_bounds__(64) void kv_append_kernel(KvAppendArgs a) {
     }
   }
 
-  // the run's box, joined with what the page's earlier tokens left
+}
+
+// The lanes' boxes of a run, and of `waves` wavefronts, joined with what the page's earlier tokens left.
+template <int D>
+__device__ inline void write_box(const KvAppendArgs &a, int64_t slot0, int h, int lane, int waves, float (*box)[2][8][64]) {
+  constexpr int OCT = D / 8, QUADS = 64 / OCT;
+  if (lane >= OCT) return;
+  uint16_t *to = a.boxes + ((slot0 / KV_PAGE * a.kv_heads + h) * 2) * (int64_t)D + lane * 8;
+  const bool begun = slot0 % KV_PAGE != 0;
+  u32x4 old[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}};
+  if (begun) {
+    old[0] = *reinterpret_cast<const u32x4 *>(to);
+    old[1] = *reinterpret_cast<const u32x4 *>(to + D);
+  }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) box[0][j][lane] = low[j], box[1][j][lane] = high[j];
-  __syncthreads();
-  if (lane < OCT) {
-    uint16_t *to = a.boxes + ((page * a.kv_heads + h) * 2) * (int64_t)D + oct * 8;
-    u32x4 old[2];
-    if (place0 != 0) {
-      old[0] = *reinterpret_cast<const u32x4 *>(to);
-      old[1] = *reinterpret_cast<const u32x4 *>(to + D);
-    }
+  for (int side = 0; side < 2; ++side) {
+    u32x4 r;
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      u32x4 r;
+    for (int j = 0; j < 8; ++j) {
+      float x = side ? -__builtin_inff() : __builtin_inff();
+      for (int w = 0; w < waves; ++w)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float x = box[side][j][lane];
-#pragma unroll
-        for (int q = 1; q < QUADS; ++q) x = side ? fmaxf(x, box[side][j][lane + q * OCT]) : fminf(x, box[side][j][lane + q * OCT]);
-        if (place0 != 0) {
-          const float was = __uint_as_float((old[side][j >> 1] >> (16 * (j & 1))) << 16);
-          x = side ? fmaxf(x, was) : fminf(x, was);
+        for (int q = 0; q < QUADS; ++q) {
+          const float y = box[w][side][j][lane + q * OCT];
+          x = side ? fmaxf(x, y) : fminf(x, y);
         }
-        const uint32_t half = __float_as_uint(x) >> 16;  // exact: two significant bits
-        r[j >> 1] = (j & 1) ? r[j >> 1] | (half << 16) : half;
+      if (begun) {
+        const float was = __uint_as_float((old[side][j >> 1] >> (16 * (j & 1))) << 16);
+        x = side ? fmaxf(x, was) : fminf(x, was);
       }
-      *reinterpret_cast<u32x4 *>(to + side * D) = r;
+      const uint32_t half = __float_as_uint(x) >> 16;  // exact: two significant bits
+      r[j >> 1] = (j & 1) ? r[j >> 1] | (half << 16) : half;
+    }
+    *reinterpret_cast<u32x4 *>(to + side * D) = r;
+  }
+}
+
+// A workgroup has the runs that begin among `tile` tokens of the list, one head.  Long runs are written by its
+// four wavefronts together, all of a page's loads in flight at once; short ones by a wavefront each.
+template <int D, int DT>
+__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a, int tile) {
+  __shared__ float box[4][2][8][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.y;
+  const int64_t i0 = (int64_t)blockIdx.x * tile;
+  // the tile's tokens that are the first of their run: all wavefronts look
+  bool first = false;
+  if (lane < tile && i0 + lane < a.tokens) {
+    const int64_t s = a.slots[i0 + lane];
+    first = s >= 0 && s < a.n_slots && (s % KV_PAGE == 0 || i0 + lane == 0 || a.slots[i0 + lane - 1] != s - 1);
+  }
+  uint64_t heads = __ballot(first);
+  float low[8], high[8];
+  auto keep = [&](int w) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) box[w][0][j][lane] = low[j], box[w][1][j][lane] = high[j];
+  };
+  for (int run = 0; heads != 0; ++run, heads &= heads - 1) {
+    const int64_t i = i0 + __builtin_ctzll(heads);
+    const int64_t slot0 = a.slots[i];
+    // its length: a lane looks at each further place of the page
+    const bool on = lane < KV_PAGE - (int)(slot0 % KV_PAGE) && i + lane < a.tokens && a.slots[i + lane] == slot0 + lane;
+    const uint64_t miss = ~__ballot(on);
+    const int n = miss ? __builtin_ctzll(miss) : 64;
+    if (n > 16) {
+      write_run<D, DT>(a, i, slot0, n, h, lane, wave, 4, low, high);
+      keep(wave);
+      __syncthreads();
+      if (wave == 0) write_box<D>(a, slot0, h, lane, 4, box);
+      __syncthreads();
+    } else if ((run & 3) == wave) {
+      write_run<D, DT>(a, i, slot0, n, h, lane, 0, 1, low, high);
+      keep(wave);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      write_box<D>(a, slot0, h, lane, 1, box + wave);
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
@@ -219,9 +258,11 @@ __global__ __launch_bounds__(64) void kv_append_kernel(KvAppendArgs a) {
 
 template <int D>
 static void append_of(const KvAppendArgs &a, int dtype, hipStream_t s) {
-  const dim3 grid((unsigned)a.tokens, (unsigned)a.kv_heads);
-  if (dtype == IVFPQ_KV_BF16) hipLaunchKernelGGL((kv_append_kernel<D, IVFPQ_KV_BF16>), grid, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL((kv_append_kernel<D, IVFPQ_KV_FP16>), grid, dim3(64), 0, s, a);
+  // few tokens: a wavefront for each, should they be runs of one; many: most are not the first of their run
+  const int tile = a.tokens <= 2048 ? 4 : 16;
+  const dim3 grid((unsigned)((a.tokens + tile - 1) / tile), (unsigned)a.kv_heads);
+  if (dtype == IVFPQ_KV_BF16) hipLaunchKernelGGL((kv_append_kernel<D, IVFPQ_KV_BF16>), grid, dim3(256), 0, s, a, tile);
+  else hipLaunchKernelGGL((kv_append_kernel<D, IVFPQ_KV_FP16>), grid, dim3(256), 0, s, a, tile);
 }
 
 int launch_kv_append(const KvAppendArgs &a, int D, int dtype, hipStream_t s) {

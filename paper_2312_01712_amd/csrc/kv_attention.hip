@@ -446,65 +446,70 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
   }
 }
 
-// Units that several workgroups share: one workgroup each adds up their parts.
+// Units that several workgroups share.  Workgroup (w, row) looks whether a unit goes across the border between
+// shares w and w + 1 and, at the first border of a unit, adds up the parts of one row: every share has a
+// lane group of its own for each D / 4 lanes, so that a context that the whole chip shares is joined in
+// a few trips to memory (520 001 tokens, 64 shares a unit: 40 us with a thread a row and 8 channels, now 4).
 template <int D, int DT, bool SEL>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
-  const int tid = threadIdx.x, row = tid >> 4, part = tid & 15;
+  constexpr int LANES = D / 4, PARTS = 256 / LANES;  // 96 channels: 24 lanes, 10 parts, 16 threads idle
+  __shared__ float red_m[4];
+  __shared__ f32x4 red_o[PARTS][LANES];
+  __shared__ float red_l[PARTS];
+  const int tid = threadIdx.x, row = blockIdx.y;
   const int64_t total = a.prefix[a.requests], span = a.prefix[a.requests + 1];
-  Unit u;
+  const int64_t border = ((int64_t)blockIdx.x + 1) * span;
+  if (border >= total) return;
   int64_t offset;
-  if constexpr (SEL) {
-    const int64_t at = (int64_t)blockIdx.x * a.n_select;
-    if (at >= total) return;
-    u = unit_at<true>(a, nullptr, at, offset);
-  } else {
-    // tiles of request r begin at q_start[r] * G / 16 + r
-    const int64_t b = blockIdx.x / a.kv_heads;
-    int lo = 0, hi = a.requests;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if ((int64_t)a.q_start[mid] * a.group / 16 + mid <= b) lo = mid;
-      else hi = mid;
-    }
-    const int fresh = min(a.q_start[lo + 1], a.tokens) - a.q_start[lo];
-    const int64_t tiles = ((int64_t)fresh * a.group + 15) / 16, tile = b - ((int64_t)a.q_start[lo] * a.group / 16 + lo);
-    if (fresh <= 0 || tile >= tiles) return;
-    const int n = request_pages(a.kv_lens[lo], fresh, a.window, a.width).n;
-    u = unit_at<false>(a, a.prefix, a.prefix[lo] + ((blockIdx.x % a.kv_heads) * tiles + tile) * n, offset);
-  }
-  const int64_t w0 = u.first / span, w1 = (u.first + u.pages - 1) / span;
-  if (w0 == w1) return;
+  const Unit u = unit_at<SEL>(a, a.prefix, border, offset);
+  if (offset == 0 || u.first < border - span) return;  // no unit across it, or not its first border
   const int rows = min(16, u.fresh * a.group - u.tile * 16);
   if (row >= rows) return;
+  const int64_t w0 = u.first / span, n = (u.first + u.pages - 1) / span - w0 + 1;
   // a workgroup's first unit is in its slot 0
-  auto slot = [&](int64_t w) { return 2 * w + (w == w0 && u.first != w0 * span); };
-  float m = -__builtin_inff(), l = 0.0f;
-  for (int64_t w = w0; w <= w1; ++w) m = fmaxf(m, a.part_ml[(slot(w) * 16 + row) * 2]);
+  auto slot = [&](int64_t k) { return 2 * (w0 + k) + (k == 0 && u.first != w0 * span); };
+  float m = -__builtin_inff();
+  for (int64_t k = tid; k < n; k += 256) m = fmaxf(m, a.part_ml[(slot(k) * 16 + row) * 2]);
+  for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  if ((tid & 63) == 0) red_m[tid >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
   const float base = m == -__builtin_inff() ? 0.0f : m;
-  float x[D / 16];
+  const int part = tid / LANES, lane = tid % LANES;
+  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+  float l = 0.0f;
+  if (part < PARTS) {
+#pragma unroll 4
+    for (int64_t k = part; k < n; k += PARTS) {
+      const int64_t at = slot(k) * 16 + row;
+      const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - base);
+      l += f * a.part_ml[at * 2 + 1];
+      x += f * *reinterpret_cast<const f32x4 *>(a.part_o + at * D + lane * 4);
+    }
+    red_o[part][lane] = x;
+    if (lane == 0) red_l[part] = l;
+  }
+  __syncthreads();
+  if (part > 0) return;
 #pragma unroll
-  for (int c = 0; c < D / 16; ++c) x[c] = 0.0f;
-  for (int64_t w = w0; w <= w1; ++w) {
-    const int64_t at = slot(w) * 16 + row;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - base);
-    l += f * a.part_ml[at * 2 + 1];
-    const float *o = a.part_o + at * D + part * (D / 16);
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) x[c] += f * o[c];
+  for (int p = 1; p < PARTS; ++p) {
+    x += red_o[p][lane];
+    l += red_l[p];
   }
   const int i = u.tile * 16 + row;
   const int64_t t = u.t0 + i / a.group;
   const int hq = u.head * a.group + i % a.group;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-  for (int c = 0; c < D / 16; ++c) x[c] *= inv;
-  store_row<DT>(a.out + t * a.out_token + hq * a.out_head + part * (D / 16), x, D / 16);
-  if (a.lse && part == 0)
+  u32x2 r;
+  r[0] = KvType<DT>::pack(x[0] * inv, x[1] * inv);
+  r[1] = KvType<DT>::pack(x[2] * inv, x[3] * inv);
+  *reinterpret_cast<u32x2 *>(a.out + t * a.out_token + hq * a.out_head + lane * 4) = r;
+  if (a.lse && lane == 0)
     a.lse[t * (a.kv_heads * a.group) + hq] = l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
 
 template <int D, int DT, bool SEL>
-int attention_of(KvAttnArgs a, int64_t units, hipStream_t s) {
+int attention_of(KvAttnArgs a, hipStream_t s) {
   a.scanned = !SEL && a.requests > SCAN_REQUESTS;
   if (a.scanned) {
     hipLaunchKernelGGL(kv_scan_kernel, dim3(1), dim3(256), 0, s, a);
@@ -515,17 +520,18 @@ int attention_of(KvAttnArgs a, int64_t units, hipStream_t s) {
                                  hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
   hipLaunchKernelGGL((kv_rows16_kernel<D, DT, SEL>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
   KV_HIP_TRY(hipGetLastError());
-  if (units == 0 || a.requests == 0) return IVFPQ_OK;
-  hipLaunchKernelGGL((kv_join_kernel<D, DT, SEL>), dim3((unsigned)units), dim3(256), 0, s, a);
+  if (a.n_wg == 1) return IVFPQ_OK;
+  const int rows = (int)(a.tokens * (int64_t)a.group < 16 ? a.tokens * (int64_t)a.group : !SEL || a.group > 16 ? 16 : a.group);
+  hipLaunchKernelGGL((kv_join_kernel<D, DT, SEL>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a);
   KV_HIP_TRY(hipGetLastError());
   return IVFPQ_OK;
 }
 
 template <int D>
-int attention_typed(const KvAttnArgs &a, int dtype, int64_t units, hipStream_t s) {
+int attention_typed(const KvAttnArgs &a, int dtype, hipStream_t s) {
   if (dtype == IVFPQ_KV_BF16)
-    return a.selected ? attention_of<D, IVFPQ_KV_BF16, true>(a, units, s) : attention_of<D, IVFPQ_KV_BF16, false>(a, units, s);
-  return a.selected ? attention_of<D, IVFPQ_KV_FP16, true>(a, units, s) : attention_of<D, IVFPQ_KV_FP16, false>(a, units, s);
+    return a.selected ? attention_of<D, IVFPQ_KV_BF16, true>(a, s) : attention_of<D, IVFPQ_KV_BF16, false>(a, s);
+  return a.selected ? attention_of<D, IVFPQ_KV_FP16, true>(a, s) : attention_of<D, IVFPQ_KV_FP16, false>(a, s);
 }
 
 struct Shape {
@@ -565,10 +571,10 @@ int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *works
   a.part_ml = reinterpret_cast<float *>(workspace + sh.prefix);
   a.part_o = reinterpret_cast<float *>(workspace + sh.prefix + sh.ml);
   switch (D) {
-    case 64: return attention_typed<64>(a, dtype, sh.units, s);
-    case 96: return attention_typed<96>(a, dtype, sh.units, s);
-    case 128: return attention_typed<128>(a, dtype, sh.units, s);
-    default: return attention_typed<256>(a, dtype, sh.units, s);
+    case 64: return attention_typed<64>(a, dtype, s);
+    case 96: return attention_typed<96>(a, dtype, s);
+    case 128: return attention_typed<128>(a, dtype, s);
+    default: return attention_typed<256>(a, dtype, s);
   }
 }
 

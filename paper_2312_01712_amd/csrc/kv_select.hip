@@ -10,8 +10,8 @@
 // kv_score_kernel: bound by the boxes, 4 D bytes a page and head; a wavefront has 16 pages, a lane
 // 16 channels of one page per step of 64, rounds them to bytes itself (the boxes stay in bf16, where
 // they are exact, so that they can grow token by token) and feeds them as they are.
-// kv_pick_kernel: one workgroup per token and head finds the n-th largest key by four counts of 8 bits
-// and writes the pages above it in order.
+// kv_pick_kernel: one workgroup per token and head finds the n-th largest key and writes the pages above it
+// in order.
 
 #include "kv_internal.h"
 
@@ -19,154 +19,175 @@ namespace ivfpq {
 
 namespace {
 
-constexpr int SCORE_WAVES = 4;
-constexpr int SCORE_PAGES = 16 * SCORE_WAVES;  // pages of a workgroup at a time
+constexpr int SCORE_PAGES = 64;  // pages of a workgroup at a time, 16 a wavefront
 
-// Rows of a tile: 16 / GP tokens of one request, GP query heads each (the group's, padded to a power
-// of two with its first head).  Groups above 16 heads go through several tiles of one token.
+// A lane's share of the box of one page: 16 channels of every 64 of [lo | hi].
+template <int D>
+struct Box {
+  u32x4 w[2 * D / 64][2];
+};
+
+template <int D>
+__device__ inline void load_box(Box<D> &b, const uint16_t *at, bool there) {
+#pragma unroll
+  for (int s = 0; s < 2 * D / 64; ++s) {
+    b.w[s][0] = b.w[s][1] = u32x4{0, 0, 0, 0};
+    if (there) {
+      b.w[s][0] = *reinterpret_cast<const u32x4 *>(at + s * 64);
+      b.w[s][1] = *reinterpret_cast<const u32x4 *>(at + s * 64 + 8);
+    }
+  }
+}
+
+// Products of 16 rows with the boxes of 16 pages; e: the exponent of a page's unit, plus 6 + 127.
+template <int D>
+__device__ inline i32x4 box_products(const Box<D> &b, const i32x4 *qa, int lane, int &e) {
+  uint32_t top = 0;  // exponent of the page's largest corner: the four lanes of a page together
+#pragma unroll
+  for (int s = 0; s < 2 * D / 64; ++s)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t w = b.w[s][j >> 2][j & 3] & 0x7fff7fffu;
+      top = max(top, max(w >> 16, w & 0xffffu));
+    }
+  top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  e = (int)(top >> 7);
+  e = e < 8 ? 8 : e;
+  const float inv = __uint_as_float((uint32_t)(260 - e) << 23);
+  i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+  for (int s = 0; s < 2 * D / 64; ++s) {
+    // rounded away from the middle: down in the first half of the row, up in the second
+    const bool up = s * 64 + (lane >> 4) * 16 >= D;
+    const float f = up ? -inv : inv;
+    i32x4 x;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t word = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = w * 4 + j;
+        const uint32_t two = b.w[s][at >> 3][(at & 7) >> 1];
+        const float c = __uint_as_float((at & 1) ? two & 0xffff0000u : two << 16);
+        int v = (int)floorf(c * f);
+        v = up ? -v : v;
+        word |= ((uint32_t)v & 255u) << (8 * j);
+      }
+      x[w] = (int)word;
+    }
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[s], x, acc, 0, 0, 0);
+  }
+  return acc;
+}
+
+// Rows of a tile: 16 / GP tokens that follow each other, GP query heads each (the group's, padded to a
+// power of two with its first head; above 16 heads one token, 16 heads at a time).  Tokens of different
+// requests in a tile are scored one request after the other.
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_score_kernel(KvSelectArgs a, int GP, int chunk) {
-  constexpr int KSTEPS = 2 * D / 64;
+  constexpr int KSTEPS = 2 * D / 64, C = D / 16;  // channels that a thread rounds
   __shared__ __attribute__((aligned(16))) int8_t rows[16][2 * D + 16];
   __shared__ float tops[16];
-  __shared__ int which;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = blockIdx.y;
-  const int tpt = GP >= 16 ? 1 : 16 / GP;  // tokens of a tile
-  // tile -> request: tiles of request r begin at q_start[r] / tpt + r
-  if (tid == 0) {
-    int lo = 0, hi = a.requests;  // last r whose first tile is not behind this one
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.q_start[mid] / tpt + mid <= (int)blockIdx.x) lo = mid;
-      else hi = mid;
-    }
-    which = lo;
-  }
-  __syncthreads();
-  const int r = which;
-  const int q0 = a.q_start[r], q1 = a.q_start[r + 1];
-  const int t0 = q0 + ((int)blockIdx.x - (q0 / tpt + r)) * tpt;
-  const int nt = min(tpt, min(q1, a.tokens) - t0);
-  if (t0 < max(q0, 0) || nt <= 0) return;
-  const int pos_last = a.positions[t0 + nt - 1];
-  const int visible = pos_last < 0 ? 0 : min(pos_last / KV_PAGE + 1, a.width);
-  const int p0 = blockIdx.z * chunk, p1 = min(p0 + chunk, visible);
-  if (p0 >= p1) return;
-  const int32_t *table = a.table + (int64_t)r * a.width;
+  const int tpt = 16 / GP;
+  const int t0 = blockIdx.x * tpt, nt = min(tpt, a.tokens - t0);
+  const int row = tid >> 4, part = tid & 15;
 
   for (int g0 = 0; g0 < a.group; g0 += 16) {  // once, unless a group has more than 16 heads
-    __syncthreads();
-    // largest query value of a token and its group: 16 threads a row
-    {
-      const int row = tid >> 4, part = tid & 15;
-      const int t = t0 + min(row / GP, nt - 1);
-      float top = 0.0f;
-      if (GP < 16 || row == 0) {
-        if (row % GP == 0)
-          for (int g = 0; g < a.group; ++g)
-            for (int c = part; c < D; c += 16) {
-              const uint16_t u = a.q[t * a.q_token + (int64_t)(h * a.group + g) * a.q_head + c];
-              if (!KvType<DT>::not_finite(u)) top = fmaxf(top, fabsf(KvType<DT>::to_float(u)));
-            }
-      }
-      for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-      if (part == 0 && row % GP == 0) tops[row / GP] = top;
-    }
-    __syncthreads();
-    {
-      const int row = tid >> 4, part = tid & 15;
+    // the rows in 8 bits, by the largest value of a token's whole group
+    float x[C], top = 0.0f;
+    for (int pass = a.group > 16 ? 0 : g0; pass <= g0 || (a.group > 16 && pass < a.group + 16); pass += 16) {
+      // groups above 16 heads: all heads for the largest value, then those of this turn
+      const bool turn = a.group <= 16 || pass >= a.group;
+      const int first = turn ? g0 : pass;
       const int tok = min(row / GP, nt - 1);
-      int g = g0 + row % GP;
-      if (g >= a.group) g = g0;
-      float scale = 127.0f * (1.0f / tops[tok]);
-      if (!(fabsf(scale) < __builtin_inff())) scale = 0.0f;
-      for (int c = part; c < D; c += 16) {
-        const uint16_t u = a.q[(int64_t)(t0 + tok) * a.q_token + (int64_t)(h * a.group + g) * a.q_head + c];
-        int v = 0;
-        if (!KvType<DT>::not_finite(u)) v = (int)rintf(KvType<DT>::to_float(u) * scale);
-        rows[row][c] = (int8_t)(v < 0 ? v : 0);
-        rows[row][D + c] = (int8_t)(v > 0 ? v : 0);
+      int g = first + row % GP;
+      if (g >= a.group) g = first;
+      const uint32_t *p = reinterpret_cast<const uint32_t *>(a.q + (int64_t)(t0 + tok) * a.q_token +
+                                                             (int64_t)(h * a.group + g) * a.q_head + part * C);
+#pragma unroll
+      for (int c = 0; c < C; c += 2) {
+        const uint32_t w = p[c / 2];
+        const uint16_t u0 = (uint16_t)w, u1 = (uint16_t)(w >> 16);
+        x[c] = KvType<DT>::not_finite(u0) ? 0.0f : KvType<DT>::to_float(u0);
+        x[c + 1] = KvType<DT>::not_finite(u1) ? 0.0f : KvType<DT>::to_float(u1);
+        top = fmaxf(top, fmaxf(fabsf(x[c]), fabsf(x[c + 1])));
       }
+      if (turn) break;
+    }
+    for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    __syncthreads();
+    if (part == 0) tops[row] = top;
+    __syncthreads();
+    for (int k = row / GP * GP; k < row / GP * GP + GP; ++k) top = fmaxf(top, tops[k]);
+    float scale = 127.0f * (1.0f / top);
+    if (!(fabsf(scale) < __builtin_inff())) scale = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int v = (int)rintf(x[c] * scale);
+      rows[row][part * C + c] = (int8_t)(v < 0 ? v : 0);
+      rows[row][D + part * C + c] = (int8_t)(v > 0 ? v : 0);
     }
     __syncthreads();
     i32x4 qa[KSTEPS];
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) qa[s] = *reinterpret_cast<const i32x4 *>(&rows[lane & 15][s * 64 + (lane >> 4) * 16]);
 
-    for (int pb = p0 + wave * 16; pb < p1; pb += SCORE_PAGES) {
-      const int col = pb + (lane & 15);
-      const int32_t page = col < p1 ? table[col] : -1;
-      const bool there = (uint32_t)page < (uint64_t)a.n_pages;
-      u32x4 box[KSTEPS][2];
+    for (int k0 = 0, k1; k0 < nt; k0 = k1) {  // tokens k0 .. k1 of one request
+      const int r = a.token_req[t0 + k0];
+      for (k1 = k0 + 1; k1 < nt && a.token_req[t0 + k1] == r; ++k1) {}
+      if ((uint32_t)r >= (uint32_t)a.requests) continue;
+      const int pos_last = a.positions[t0 + k1 - 1];
+      const int visible = pos_last < 0 ? 0 : min(pos_last / KV_PAGE + 1, a.width);
+      const int p0 = blockIdx.z * chunk, p1 = min(p0 + chunk, visible);
+      const int32_t *table = a.table + (int64_t)r * a.width;
+      // two tiles of pages ahead: their numbers, and one box
+      auto number = [&](int pb) -> int32_t {
+        const int col = pb + (lane & 15);
+        return col < p1 ? table[col] : -1;
+      };
+      auto fetch = [&](Box<D> &b, int32_t page) {
+        const bool there = (uint32_t)page < (uint64_t)a.n_pages;
+        load_box<D>(b, a.boxes + ((int64_t)(there ? page : 0) * a.kv_heads + h) * (2 * D) + (lane >> 4) * 16, there);
+      };
+      auto finish = [&](const Box<D> &b, int pb, int32_t page) {
+        int e;
+        const i32x4 acc = box_products<D>(b, qa, lane, e);
+        // the lane has rows 4 (lane / 16) .. + 3 of its page: the largest of each token's
+        const bool there = (uint32_t)page < (uint64_t)a.n_pages;
+        const float unit = __uint_as_float((uint32_t)(e - 6) << 23);
+        int best[4] = {acc[0], acc[1], acc[2], acc[3]};
+        if (GP >= 2) best[0] = max(best[0], best[1]), best[2] = max(best[2], best[3]);
+        if (GP >= 4) best[0] = max(best[0], best[2]);
+        if (GP >= 8) best[0] = max(best[0], __shfl_xor(best[0], 16));
+        if (GP >= 16) best[0] = max(best[0], __shfl_xor(best[0], 32));
+        const int col = pb + (lane & 15);
 #pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) {
-        box[s][0] = u32x4{0, 0, 0, 0};
-        box[s][1] = u32x4{0, 0, 0, 0};
-      }
-      if (there) {
-        const uint16_t *b = a.boxes + ((int64_t)page * a.kv_heads + h) * (2 * D) + (lane >> 4) * 16;
-#pragma unroll
-        for (int s = 0; s < KSTEPS; ++s) {
-          box[s][0] = *reinterpret_cast<const u32x4 *>(b + s * 64);
-          box[s][1] = *reinterpret_cast<const u32x4 *>(b + s * 64 + 8);
-        }
-      }
-      // exponent of the page's largest corner: the four lanes of a page together
-      uint32_t top = 0;
-#pragma unroll
-      for (int s = 0; s < KSTEPS; ++s)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t w = box[s][j >> 2][j & 3] & 0x7fff7fffu;
-          top = max(top, max(w >> 16, w & 0xffffu));
-        }
-      top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-      int e = (int)(top >> 7);
-      e = e < 8 ? 8 : e;
-      const float inv = __uint_as_float((uint32_t)(260 - e) << 23);
-      i32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) {
-        // rounded away from the middle: down in the first half of the row, up in the second
-        const bool up = s * 64 + (lane >> 4) * 16 >= D;
-        const float f = up ? -inv : inv;
-        i32x4 b;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          uint32_t word = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int at = w * 4 + j;
-            const uint32_t two = box[s][at >> 3][(at & 7) >> 1];
-            const float x = __uint_as_float((at & 1) ? two & 0xffff0000u : two << 16);
-            int v = (int)floorf(x * f);
-            v = up ? -v : v;
-            word |= ((uint32_t)v & 255u) << (8 * j);
+        for (int i = 0; i < 4; ++i) {
+          const int at = (lane >> 4) * 4 + i, k = at / GP;
+          if (at % GP == 0 && k >= k0 && k < k1 && col < p1) {
+            float *to = a.scores + ((int64_t)(t0 + k) * a.kv_heads + h) * a.score_width + col;
+            float s = there ? (float)best[i] * unit : -__builtin_inff();
+            if (g0 > 0) s = fmaxf(s, *to);
+            *to = s;
           }
-          b[w] = (int)word;
         }
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[s], b, acc, 0, 0, 0);
-      }
-      // the lane has rows 4 (lane / 16) .. + 3 of its page: the largest of each token's
-      const float unit = __uint_as_float((uint32_t)(e - 6) << 23);
-      const int first = (lane >> 4) * 4;
-      int best[4] = {acc[0], acc[1], acc[2], acc[3]};
-      if (GP >= 2) best[0] = max(best[0], best[1]), best[2] = max(best[2], best[3]);
-      if (GP >= 4) best[0] = max(best[0], best[2]);
-      if (GP >= 8) best[0] = max(best[0], __shfl_xor(best[0], 16));
-      if (GP >= 16) best[0] = max(best[0], __shfl_xor(best[0], 32));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = first + i;
-        if (row % GP == 0 && row / GP < nt && col < p1) {
-          const int t = t0 + row / GP;
-          float *to = a.scores + ((int64_t)t * a.kv_heads + h) * a.score_width + col;
-          float s = there ? (float)best[i] * unit : -__builtin_inff();
-          if (g0 > 0) s = fmaxf(s, *to);
-          *to = s;
-        }
+      };
+      Box<D> even, odd;
+      int pb = p0 + wave * 16;
+      int32_t page = number(pb), next = number(pb + SCORE_PAGES);
+      if (pb < p1) fetch(even, page);
+      for (; pb < p1; pb += 2 * SCORE_PAGES) {
+        const int32_t third = number(pb + 2 * SCORE_PAGES), fourth = number(pb + 3 * SCORE_PAGES);
+        fetch(odd, next);
+        finish(even, pb, page);
+        if (pb + SCORE_PAGES >= p1) break;
+        fetch(even, third);
+        finish(odd, pb + SCORE_PAGES, next);
+        page = third;
+        next = fourth;
       }
     }
   }
@@ -178,11 +199,34 @@ __device__ inline uint32_t key_of(float s) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-constexpr int PICK_THREADS = 256;
+constexpr int PICK_BINS = 2048;
 
-__global__ __launch_bounds__(PICK_THREADS) void kv_pick_kernel(KvSelectArgs a) {
-  __shared__ int counts[256];
-  __shared__ int sums[2][PICK_THREADS / 64];
+// Inclusive sums over the workgroup, in thread order.
+template <int THREADS>
+__device__ inline int block_sum(int x, int *sums, int tid) {
+  const int lane = tid & 63, wave = tid >> 6;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(x, d);
+    if (lane >= d) x += u;
+  }
+  __syncthreads();  // the sums of a call before are read
+  if (lane == 63) sums[wave] = x;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) x += sums[w];
+  return x;
+}
+
+// The columns of one token and head, four a thread and turn.  The n-th largest key: counts of the keys in
+// 2048 bins between the smallest and the largest (the scores of a context lie within a few octaves,
+// so that bins of equal width spread them), then again within the bin that holds it, 11 bits a time.
+// Up to TURNS * 4 * THREADS columns keep their keys in registers, more are read again.
+// Bound by the latency of its few dependent steps (4094 columns: 20.7 us with four counts of 8 bits, whose
+// first digit is the same for all).
+template <int THREADS, int TURNS>
+__global__ __launch_bounds__(THREADS) void kv_pick_kernel(KvSelectArgs a) {
+  __shared__ int counts[PICK_BINS];
+  __shared__ int sums[THREADS / 64];
+  __shared__ uint32_t range[2][THREADS / 64];
   __shared__ int found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.x;
@@ -192,77 +236,103 @@ __global__ __launch_bounds__(PICK_THREADS) void kv_pick_kernel(KvSelectArgs a) {
   // a page number beyond the request's own is never asked for
   const int visible = (uint32_t)r < (uint32_t)a.requests && pos >= 0 ? min(pos / KV_PAGE + 1, a.width) : 0;
   if (visible <= n) {
-    for (int i = tid; i < n; i += PICK_THREADS) out[i] = i < visible ? i : -1;
+    for (int i = tid; i < n; i += THREADS) out[i] = i < visible ? i : -1;
     return;
   }
   const float *scores = a.scores + (t * a.kv_heads + h) * (int64_t)a.score_width;
-  auto key_at = [&](int i) -> uint32_t {
-    if (i < a.sinks || i >= visible - a.recent) return 0xffffffffu;
-    return key_of(scores[i]);
+  // columns i .. i + 3 (rows of scores are padded to four); which of them are ranked
+  auto load = [&](int i, uint32_t (&k)[4]) {
+    const f32x4 s = i < visible ? *reinterpret_cast<const f32x4 *>(scores + i) : f32x4{0, 0, 0, 0};
+    for (int j = 0; j < 4; ++j) k[j] = key_of(s[j]);
   };
-  // the n-th largest key, eight bits at a time
-  uint32_t prefix = 0, mask = 0;
-  int left = n;  // how many of the keys that share the prefix are wanted
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    counts[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < visible; i += PICK_THREADS) {
-      const uint32_t k = key_at(i);
-      if ((k & mask) == prefix) atomicAdd(&counts[(k >> shift) & 255], 1);
+  auto ranked = [&](int i) { return i >= a.sinks && i < visible - a.recent; };
+  uint32_t kept[TURNS][4];
+#pragma unroll
+  for (int m = 0; m < TURNS; ++m) load((m * THREADS + tid) * 4, kept[m]);
+  // every column, in order of turns; f(first column, keys)
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int m = 0; m < TURNS; ++m)
+      if (m * THREADS * 4 < visible) f((m * THREADS + tid) * 4, kept[m]);
+    for (int b = TURNS * THREADS * 4; b < visible; b += THREADS * 4) {
+      uint32_t k[4];
+      load(b + tid * 4, k);
+      f(b + tid * 4, k);
     }
-    __syncthreads();
-    // from the largest digit down: the digit at which the count reaches `left`
-    if (wave == 0) {
-      int c[4], sum = 0;
+  };
+  uint32_t lo = 0xffffffffu, hi = 0;
+  each([&](int i, const uint32_t (&k)[4]) {
+    for (int j = 0; j < 4; ++j)
+      if (ranked(i + j)) lo = min(lo, k[j]), hi = max(hi, k[j]);
+  });
+  for (int d = 32; d > 0; d >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, d));
+  }
+  if (lane == 0) range[0][wave] = lo, range[1][wave] = hi;
+  __syncthreads();
+  for (int w = 0; w < THREADS / 64; ++w) lo = min(lo, range[0][w]), hi = max(hi, range[1][w]);
+  // keys above `limit` are in, and of those equal to it the first `left`
+  int left = n - a.sinks - a.recent;
+  uint32_t limit = 0xffffffffu;
+  if (left > 0) {
+    for (;;) {
+      const uint32_t width = hi - lo;
+      const int shift = width < PICK_BINS ? 0 : 32 - __clz((int)width) - 11;
+      for (int b = tid; b < PICK_BINS; b += THREADS) counts[b] = 0;
+      __syncthreads();
+      each([&](int i, const uint32_t (&k)[4]) {
+        for (int j = 0; j < 4; ++j)
+          if (ranked(i + j) && k[j] >= lo && k[j] <= hi) atomicAdd(&counts[(k[j] - lo) >> shift], 1);
+      });
+      __syncthreads();
+      // from the highest bin down: the one at which the count reaches `left`
+      constexpr int PER = PICK_BINS / THREADS;
+      int c[PER], sum = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c[j] = counts[255 - (lane * 4 + j)], sum += c[j];
-      int before = sum;
-      for (int d = 1; d < 64; d <<= 1) {
-        const int u = __shfl_up(before, d);
-        if (lane >= d) before += u;
-      }
-      before -= sum;
+      for (int j = 0; j < PER; ++j) c[j] = counts[PICK_BINS - 1 - (tid * PER + j)], sum += c[j];
+      int before = block_sum<THREADS>(sum, sums, tid) - sum;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (before < left && before + c[j] >= left) found[0] = 255 - (lane * 4 + j), found[1] = left - before;
+      for (int j = 0; j < PER; ++j) {
+        if (before < left && before + c[j] >= left) found[0] = PICK_BINS - 1 - (tid * PER + j), found[1] = left - before;
         before += c[j];
       }
+      __syncthreads();
+      const uint32_t bin = (uint32_t)found[0];
+      left = found[1];
+      lo += bin << shift;
+      hi = min(hi, lo + ((1u << shift) - 1));
+      __syncthreads();
+      if (lo == hi) break;
     }
-    __syncthreads();
-    prefix |= (uint32_t)found[0] << shift;
-    mask |= 255u << shift;
-    left = found[1];
-    __syncthreads();
+    limit = lo;
   }
-  // in order: all above the n-th key, and the first `left` of those equal to it
-  const int per = (visible + PICK_THREADS - 1) / PICK_THREADS;
-  const int i0 = min(tid * per, visible), i1 = min(i0 + per, visible);
-  int above = 0, equal = 0;
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t k = key_at(i);
-    above += k > prefix;
-    equal += k == prefix;
-  }
-  int sa = above, se = equal;
-  for (int d = 1; d < 64; d <<= 1) {
-    const int u = __shfl_up(sa, d), v = __shfl_up(se, d);
-    if (lane >= d) sa += u, se += v;
-  }
-  if (lane == 63) sums[0][wave] = sa, sums[1][wave] = se;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) sa += sums[0][w], se += sums[1][w];
-  sa -= above;
-  se -= equal;
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t k = key_at(i);
-    if (k > prefix) {
-      out[sa + min(se, left)] = i;
-      ++sa;
-    } else if (k == prefix) {
-      if (se < left) out[sa + se] = i;
-      ++se;
-    }
-  }
+  // in order: the first and last columns, all keys above the limit, and the first `left` of those equal to it
+  int equals = 0, chosen = 0;  // before this turn
+  each([&](int i, const uint32_t (&k)[4]) {
+    int eq = 0, in = 0;
+    for (int j = 0; j < 4; ++j)
+      if (i + j < visible) {
+        const bool forced = !ranked(i + j);
+        eq += !forced && left > 0 && k[j] == limit;
+        in += forced || (left > 0 && k[j] > limit);
+      }
+    // two counts in one sum: both are below 2^15 in a turn
+    const int both = block_sum<THREADS>(in | eq << 16, sums, tid);
+    int e = equals + (both >> 16) - eq, at = chosen + (both & 0xffff) - in;
+    for (int j = 0; j < 4; ++j)
+      if (i + j < visible) {
+        const bool forced = !ranked(i + j);
+        const bool same = !forced && left > 0 && k[j] == limit;
+        if (forced || (left > 0 && k[j] > limit) || (same && e < left)) out[at + min(e, left)] = i + j;
+        if (same) ++e;
+        else at += forced || (left > 0 && k[j] > limit);
+      }
+    int last = 0;
+    for (int w = 0; w < THREADS / 64; ++w) last += sums[w];
+    equals += last >> 16;
+    chosen += last & 0xffff;
+  });
 }
 
 template <int D>
@@ -277,13 +347,10 @@ int launch_kv_select(const KvSelectArgs &a, int D, int dtype, hipStream_t s) {
   if (a.requests > 0 && a.width > a.n_select) {
     int GP = 1;
     while (GP < a.group && GP < 16) GP <<= 1;
-    const int tpt = GP >= 16 ? 1 : 16 / GP;
-    const int64_t tiles = a.tokens / tpt + a.requests;
-    // pages of a workgroup: 1024 workgroups and more where there are that many rows, 64 pages at least
-    int64_t chunk = (int64_t)a.width * tiles * a.kv_heads / 2048;
-    chunk = (chunk + SCORE_PAGES - 1) / SCORE_PAGES * SCORE_PAGES;
-    if (chunk < SCORE_PAGES) chunk = SCORE_PAGES;
-    if (chunk > 1024) chunk = 1024;
+    const int64_t tiles = (a.tokens + 16 / GP - 1) / (16 / GP);
+    // pages of a workgroup: two turns of its wavefronts, more where that would be a great many workgroups
+    int64_t chunk = 2 * SCORE_PAGES;
+    while (chunk < 1024 && tiles * a.kv_heads * ((a.width + chunk - 1) / chunk) > 16384) chunk *= 2;
     const dim3 grid((unsigned)tiles, (unsigned)a.kv_heads, (unsigned)((a.width + chunk - 1) / chunk));
     switch (D) {
       case 64: score_of<64>(a, dtype, grid, GP, (int)chunk, s); break;
@@ -293,7 +360,10 @@ int launch_kv_select(const KvSelectArgs &a, int D, int dtype, hipStream_t s) {
     }
     KV_HIP_TRY(hipGetLastError());
   }
-  hipLaunchKernelGGL(kv_pick_kernel, dim3((unsigned)a.tokens, (unsigned)a.kv_heads), dim3(PICK_THREADS), 0, s, a);
+  const dim3 grid((unsigned)a.tokens, (unsigned)a.kv_heads);
+  if (a.width <= 1024) hipLaunchKernelGGL((kv_pick_kernel<256, 1>), grid, dim3(256), 0, s, a);
+  else if (a.width <= 4096) hipLaunchKernelGGL((kv_pick_kernel<1024, 1>), grid, dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL((kv_pick_kernel<1024, 4>), grid, dim3(1024), 0, s, a);
   KV_HIP_TRY(hipGetLastError());
   return IVFPQ_OK;
 }
