@@ -24,10 +24,21 @@ constexpr int SCAN_REQUESTS = 2048;  // more than these: their units are scanned
 __device__ inline float xor16_max(float x) { return fmaxf(x, __shfl_xor(x, 16)); }
 __device__ inline float xor32_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
 
+// values that are the same in all lanes, in scalar registers
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
+}
+
 // pages [lo, lo + n) that any new token of a request sees; n >= 1
 struct Range {
   int lo, n;
 };
+
+// What a workgroup leaves about the unit that goes across the border behind its share, if it began in it:
+// shares that have some of it (0: there is none), whether it is not the first unit in its first
+// share, first token, tile, kv head, rows.
+constexpr int BORDER_INTS = 8;
 
 __device__ inline Range request_pages(int kv, int fresh, int window, int width) {
   Range g = {0, 1};
@@ -283,23 +294,23 @@ __device__ inline Unit unit_at(const KvAttnArgs &a, const int64_t *prefix, int64
     u.lo = 0, u.pages = a.n_select;
     offset = rest % a.n_select;
     u.t0 = u.g, u.fresh = 1;
-    const int r = a.token_req[u.g];
+    const int r = uniform(a.token_req[u.g]);
     u.req = (uint32_t)r < (uint32_t)a.requests ? r : -1;
-    u.kv = u.req >= 0 ? a.kv_lens[u.req] : 0;
+    u.kv = u.req >= 0 ? uniform(a.kv_lens[u.req]) : 0;
   } else {
     int lo = 0, hi = a.requests;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (prefix[mid] <= at) lo = mid;
+      if (uniform(prefix[mid]) <= at) lo = mid;
       else hi = mid;
     }
     u.g = u.req = lo;
-    u.t0 = a.q_start[lo];
-    u.fresh = min(a.q_start[lo + 1], a.tokens) - u.t0;
-    u.kv = a.kv_lens[lo];
+    u.t0 = uniform(a.q_start[lo]);
+    u.fresh = min(uniform(a.q_start[lo + 1]), a.tokens) - u.t0;
+    u.kv = uniform(a.kv_lens[lo]);
     const Range pr = request_pages(u.kv, u.fresh, a.window, a.width);
     const int tiles = (int)(((int64_t)u.fresh * a.group + 15) / 16);
-    const int64_t rest = at - prefix[lo], k = rest / pr.n;
+    const int64_t rest = at - uniform(prefix[lo]), k = rest / pr.n;
     u.head = (int)(k / tiles), u.tile = (int)(k % tiles);
     u.lo = pr.lo, u.pages = pr.n;
     offset = rest % pr.n;
@@ -354,7 +365,7 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
   float(*ml)[16][2] = reinterpret_cast<float(*)[16][2]>(buf + 4 * 16 * (D + 4));  // [4]
   int64_t *sums = reinterpret_cast<int64_t *>(ml + 4);                            // [4]
   int64_t *own_prefix = sums + 4;                                                 // [requests], dense
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4;
   const int64_t wg = blockIdx.x;
 
   clear_rest<D>(a, wg, gridDim.x, tid);
@@ -362,17 +373,11 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
   if constexpr (SEL) total = (int64_t)(a.requests > 0 ? min(a.q_start[a.requests], a.tokens) : 0) * a.kv_heads * ((a.group + 15) / 16) * a.n_select;
   else total = a.scanned ? a.prefix[a.requests] : scan_units(a, own_prefix, sums, tid);
   const int64_t *prefix = !SEL && a.scanned ? a.prefix : own_prefix;
+  total = uniform(total);
   int64_t span = (total + a.n_wg - 1) / a.n_wg;
   if (span < 4) span = 4;
-  if (wg == 0) {
-    if (!SEL && !a.scanned)
-      for (int i = tid; i < a.requests; i += 256) a.prefix[i] = own_prefix[i];
-    if (tid == 0) {
-      if (SEL || !a.scanned) a.prefix[a.requests] = total;
-      a.prefix[a.requests + 1] = span;
-    }
-  }
   const int64_t begin = wg * span, end = min(begin + span, total);
+  if (tid == 0 && begin >= end) a.borders[wg * BORDER_INTS] = 0;
   for (int64_t at = begin; at < end;) {
     int64_t offset;
     const Unit u = unit_at<SEL>(a, prefix, at, offset);
@@ -392,10 +397,10 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
       clear_low = max(clear_low, __shfl_xor(clear_low, d));
       any_low = min(any_low, __shfl_xor(any_low, d));
     }
-    clear_high = __builtin_amdgcn_readfirstlane(clear_high);
-    clear_low = __builtin_amdgcn_readfirstlane(clear_low);
-    any_high = __builtin_amdgcn_readfirstlane(any_high);
-    any_low = __builtin_amdgcn_readfirstlane(any_low);
+    clear_high = uniform(clear_high);
+    clear_low = uniform(clear_low);
+    any_high = uniform(any_high);
+    any_low = uniform(any_low);
     u32x4 qf[D / 32];
     {
       const uint16_t *qp = a.q + t * a.q_token + hq * a.q_head + g * (D / 4);
@@ -410,27 +415,49 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
 
     const int32_t *table = a.table + (int64_t)max(u.req, 0) * a.width;
     const int32_t *list = SEL ? a.selected + ((int64_t)u.t0 * a.kv_heads + u.head) * a.n_select : nullptr;
-    const int64_t head_bytes = kv_head_bytes(D);
-    // column of entry k of the unit, or -1 where no row sees anything of it
-    auto column = [&](int k) -> int {
-      int c = u.lo + k;
-      if constexpr (SEL) c = list[k];
-      if ((uint32_t)c >= (uint32_t)a.width || u.req < 0) return -1;
-      if (c * KV_PAGE > any_high || c * KV_PAGE + KV_PAGE - 1 <= any_low) return -1;
-      return c;
-    };
+    const char *heads = a.pages + u.head * (int64_t)kv_head_bytes(D);
+    const int64_t page_bytes = a.kv_heads * (int64_t)kv_head_bytes(D);
     const int k1 = (int)offset + n;
-    for (int k = (int)offset + wave; k < k1; k += 4) {
-      const int c = __builtin_amdgcn_readfirstlane(column(k));
-      if (c < 0) continue;
-      const int page = __builtin_amdgcn_readfirstlane(table[c]);
-      if ((uint32_t)page >= (uint64_t)a.n_pages) continue;
-      Page<D> pg;
-      pg.load(a.pages + ((int64_t)page * a.kv_heads + u.head) * head_bytes, lane);
-      const int first = c * KV_PAGE;
-      if (first + KV_PAGE > u.kv) pg.cut(u.kv - first, lane);
-      const bool masked = first + KV_PAGE - 1 > clear_high || first <= clear_low;
-      page_step<D, DT>(pg, qf, r, lane, a.scale2, masked, first, low, high);
+    // the wavefront's entries offset + wave, + 4, ...: a lane looks 64 of them up at a time
+    for (int k0 = (int)offset + wave; k0 < k1; k0 += 4 * 64) {
+      const int k = k0 + 4 * lane;
+      int c = -1, page = -1;
+      if (k < k1 && u.req >= 0) {
+        c = u.lo + k;
+        if constexpr (SEL) c = list[k];
+        // a column that no row sees anything of, or without a page in the cache
+        if ((uint32_t)c < (uint32_t)a.width && c * KV_PAGE <= any_high && c * KV_PAGE + KV_PAGE - 1 > any_low) page = table[c];
+      }
+      uint64_t todo = __ballot((uint32_t)page < (uint64_t)a.n_pages);
+      auto fetch = [&](Page<D> &pg, uint64_t left) {
+        pg.load(heads + __builtin_amdgcn_readlane(page, __builtin_ctzll(left)) * page_bytes, lane);
+      };
+      auto step = [&](Page<D> &pg, uint64_t left) {
+        const int first = __builtin_amdgcn_readlane(c, __builtin_ctzll(left)) * KV_PAGE;
+        if (first + KV_PAGE > u.kv) pg.cut(u.kv - first, lane);
+        const bool masked = first + KV_PAGE - 1 > clear_high || first <= clear_low;
+        page_step<D, DT>(pg, qf, r, lane, a.scale2, masked, first, low, high);
+      };
+      // a page is requested while the one before it is worked on (256 channels: no registers for two)
+      if constexpr (D <= 128) {
+        Page<D> even, odd;
+        if (todo) fetch(even, todo);
+        while (todo) {
+          const uint64_t then = todo & (todo - 1);
+          if (then) fetch(odd, then);
+          step(even, todo);
+          if (!then) break;
+          todo = then & (then - 1);
+          if (todo) fetch(even, todo);
+          step(odd, then);
+        }
+      } else {
+        for (; todo; todo &= todo - 1) {
+          Page<D> pg;
+          fetch(pg, todo);
+          step(pg, todo);
+        }
+      }
     }
     // l of the whole row
     r.l += __shfl_xor(r.l, 16);
@@ -442,34 +469,37 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
       *reinterpret_cast<f32x4 *>(buf + (wave * 16 + (lane & 15)) * (D + 4) + ct * 16 + g * 4) = r.o[ct];
     __syncthreads();
     join_waves<D, DT, SEL>(a, u, rows, n == u.pages, 2 * wg + (at != begin), ml, buf, tid);
+    if (tid == 0 && at + n == end) {
+      const bool across = u.first + u.pages > end && u.first >= begin;
+      int32_t *b = a.borders + wg * BORDER_INTS;
+      b[0] = across ? (int32_t)((u.first + u.pages - 1) / span - wg) + 1 : 0;
+      b[1] = at != begin;
+      b[2] = u.t0;
+      b[3] = u.tile;
+      b[4] = u.head;
+      b[5] = rows;
+    }
     at += n;
   }
 }
 
-// Units that several workgroups share.  Workgroup (w, row) looks whether a unit goes across the border between
-// shares w and w + 1 and, at the first border of a unit, adds up the parts of one row: every share has a
-// lane group of its own for each D / 4 lanes, so that a context that the whole chip shares is joined in
+// Units that several workgroups share.  Workgroup (w, row) adds up one row's parts of the unit that goes across
+// the border behind share w and began in it.  D / 4 lanes have a part each, so that a context that the whole chip shares is joined in
 // a few trips to memory (520 001 tokens, 64 shares a unit: 40 us with a thread a row and 8 channels, now 4).
-template <int D, int DT, bool SEL>
+template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   constexpr int LANES = D / 4, PARTS = 256 / LANES;  // 96 channels: 24 lanes, 10 parts, 16 threads idle
   __shared__ float red_m[4];
   __shared__ f32x4 red_o[PARTS][LANES];
   __shared__ float red_l[PARTS];
   const int tid = threadIdx.x, row = blockIdx.y;
-  const int64_t total = a.prefix[a.requests], span = a.prefix[a.requests + 1];
-  const int64_t border = ((int64_t)blockIdx.x + 1) * span;
-  if (border >= total) return;
-  int64_t offset;
-  const Unit u = unit_at<SEL>(a, a.prefix, border, offset);
-  if (offset == 0 || u.first < border - span) return;  // no unit across it, or not its first border
-  const int rows = min(16, u.fresh * a.group - u.tile * 16);
-  if (row >= rows) return;
-  const int64_t w0 = u.first / span, n = (u.first + u.pages - 1) / span - w0 + 1;
+  const int32_t *b = a.borders + (int64_t)blockIdx.x * BORDER_INTS;
+  const int n = b[0], late = b[1], t0 = b[2], tile = b[3], head = b[4], rows = b[5];
+  if (n == 0 || row >= rows) return;
   // a workgroup's first unit is in its slot 0
-  auto slot = [&](int64_t k) { return 2 * (w0 + k) + (k == 0 && u.first != w0 * span); };
+  auto slot = [&](int k) { return 2 * ((int64_t)blockIdx.x + k) + (k == 0 && late); };
   float m = -__builtin_inff();
-  for (int64_t k = tid; k < n; k += 256) m = fmaxf(m, a.part_ml[(slot(k) * 16 + row) * 2]);
+  for (int k = tid; k < n; k += 256) m = fmaxf(m, a.part_ml[(slot(k) * 16 + row) * 2]);
   for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
   if ((tid & 63) == 0) red_m[tid >> 6] = m;
   __syncthreads();
@@ -480,7 +510,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   float l = 0.0f;
   if (part < PARTS) {
 #pragma unroll 4
-    for (int64_t k = part; k < n; k += PARTS) {
+    for (int k = part; k < n; k += PARTS) {
       const int64_t at = slot(k) * 16 + row;
       const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - base);
       l += f * a.part_ml[at * 2 + 1];
@@ -496,9 +526,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
     x += red_o[p][lane];
     l += red_l[p];
   }
-  const int i = u.tile * 16 + row;
-  const int64_t t = u.t0 + i / a.group;
-  const int hq = u.head * a.group + i % a.group;
+  const int i = tile * 16 + row;
+  const int64_t t = t0 + i / a.group;
+  const int hq = head * a.group + i % a.group;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   u32x2 r;
   r[0] = KvType<DT>::pack(x[0] * inv, x[1] * inv);
@@ -522,7 +552,7 @@ int attention_of(KvAttnArgs a, hipStream_t s) {
   KV_HIP_TRY(hipGetLastError());
   if (a.n_wg == 1) return IVFPQ_OK;
   const int rows = (int)(a.tokens * (int64_t)a.group < 16 ? a.tokens * (int64_t)a.group : !SEL || a.group > 16 ? 16 : a.group);
-  hipLaunchKernelGGL((kv_join_kernel<D, DT, SEL>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((kv_join_kernel<D, DT>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a);
   KV_HIP_TRY(hipGetLastError());
   return IVFPQ_OK;
 }
@@ -537,7 +567,7 @@ int attention_typed(const KvAttnArgs &a, int dtype, hipStream_t s) {
 struct Shape {
   int64_t units;   // (group, head, tile), at most
   int n_wg;
-  size_t prefix, ml, o;  // bytes
+  size_t prefix, borders, ml, o;  // bytes
 };
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -548,7 +578,8 @@ Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D,
   const int64_t pages = s.units * (n_select > 0 ? n_select : width);
   // two workgroups on every CU, four pages each at least
   s.n_wg = pages / 4 >= 512 ? 512 : (int)(pages / 4 + 1);
-  s.prefix = up256((size_t)(requests + 2) * 8);
+  s.prefix = up256((size_t)(requests + 1) * 8);
+  s.borders = up256((size_t)s.n_wg * BORDER_INTS * 4);
   s.ml = up256((size_t)s.n_wg * 2 * 16 * 2 * 4);
   s.o = up256((size_t)s.n_wg * 2 * 16 * D * 4);
   return s;
@@ -560,7 +591,7 @@ size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, in
                               int64_t width) {
   (void)max_new;
   const Shape s = shape_of(tokens, requests, kv_heads, group, D, n_select, width);
-  return s.prefix + s.ml + s.o;
+  return s.prefix + s.borders + s.ml + s.o;
 }
 
 int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s) {
@@ -568,8 +599,9 @@ int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *works
   const Shape sh = shape_of(a.tokens, a.requests, a.kv_heads, a.group, D, a.selected ? a.n_select : 0, a.width);
   a.n_wg = sh.n_wg;
   a.prefix = reinterpret_cast<int64_t *>(workspace);
-  a.part_ml = reinterpret_cast<float *>(workspace + sh.prefix);
-  a.part_o = reinterpret_cast<float *>(workspace + sh.prefix + sh.ml);
+  a.borders = reinterpret_cast<int32_t *>(workspace + sh.prefix);
+  a.part_ml = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders);
+  a.part_o = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders + sh.ml);
   switch (D) {
     case 64: return attention_typed<64>(a, dtype, s);
     case 96: return attention_typed<96>(a, dtype, s);

@@ -62,7 +62,8 @@ struct KvAttnArgs {
   float scale2;  // scale * log2(e)
   // split over pages: workgroup w takes [w, w + 1) * span of the (group, head, tile, page) units in order
   int32_t n_wg, scanned;
-  int64_t *prefix;  // [groups + 1]: units before a group, then the span (written by the scan, read by the join)
+  int64_t *prefix;   // [requests + 1]: units before each request, where a launch of its own scans them
+  int32_t *borders;  // [n_wg][8]: the unit that goes on in the next share
   float *part_ml;   // [2 n_wg][rows][2]
   float *part_o;    // [2 n_wg][rows][D]
 };
