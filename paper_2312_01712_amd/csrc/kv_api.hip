@@ -108,7 +108,8 @@ int check_attention(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, const ivfpq
   if (a->max_new < 1 && s->max_tokens > 0) return invalid(fn, "max_new must be positive");
   // the launch's grid has a workgroup per token, kv head and 16 heads of a group
   const int64_t group = a->heads / c->kv_heads;
-  if (((int64_t)s->max_tokens * ((group + 15) / 16) + s->requests) * c->kv_heads > 0x7fffffff) {
+  if (((int64_t)s->max_tokens * ((group + 15) / 16) + s->requests) * c->kv_heads > 0x7fffffff ||
+      (int64_t)s->max_tokens * group > 0x7fffffff) {
     set_error("%s: max_tokens * heads is too large for one launch", fn);
     return IVFPQ_ERR_UNSUPPORTED;
   }
@@ -247,7 +248,10 @@ int ivfpq_kv_attention(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, const iv
   a.token_req = s->token_req; a.positions = s->positions; a.selected = x->selected; a.q_token = x->q.token_stride;
   a.q_head = x->q.head_stride; a.out_token = x->out_token_stride; a.out_head = x->out_head_stride; a.n_pages = c->n_pages;
   a.kv_heads = c->kv_heads; a.group = group; a.requests = s->requests; a.tokens = s->max_tokens; a.width = s->table_width;
-  a.n_select = x->n_select; a.window = x->window; a.scale2 = x->scale * 1.44269504088896340736f;
+  a.n_select = x->n_select; a.window = x->window; 
+  // 0 as the smallest number above it: masked keys are -inf, which 0 would turn into NaN
+  a.negative = x->scale < 0.0f;
+  a.scale2 = fmaxf(fabsf(x->scale) * 1.44269504088896340736f, 1.17549435e-38f);
   return launch_kv_attention(a, c->head_dim, c->dtype, x->max_new, static_cast<char *>(d_workspace),
                              static_cast<hipStream_t>(stream));
 }

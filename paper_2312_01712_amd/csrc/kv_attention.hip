@@ -6,10 +6,14 @@
 // rounded to the cache's type for the second product (as the values are: both factors exact or
 // within half a unit of the result's type).
 //
-// Layout.  A wavefront has 16 rows (query heads of one kv head, tokens above them) and works on
-// S^T = K Q^T and O^T = V^T P^T, so that a lane holds one row's statistics and the exponentials
-// of the first product are, in place, the second operand of the second: lane (g, row) has keys
-// 16 tt + 4 g + i, and the page stores the values in this order of tokens.
+// Layout.  A wavefront works on S^T = K Q^T and O^T = V^T P^T, 16 rows (query heads of one kv head, tokens above
+// them) at a time, so that a lane holds one row's statistics and the exponentials of the first
+// product are, in place, the second operand of the second: lane (g, row) has keys 16 tt + 4 g + i, and
+// the page stores the values in this order of tokens.
+//
+// Two kernels.  kv_rows16_kernel: 16 rows or fewer share a page (decode, selected pages); its wavefronts have
+// pages of their own, held in registers from memory to the products.  kv_rows_kernel: many rows share a
+// page (chunks of prompts); a workgroup unpacks a page into LDS once and its wavefronts have 32 rows each.
 
 #include <type_traits>
 
@@ -19,10 +23,22 @@ namespace ivfpq {
 
 namespace {
 
-constexpr int SCAN_REQUESTS = 2048;  // more than these: their units are scanned by a launch of its own
+constexpr int SCAN_REQUESTS = 512;  // more than these: their units are scanned by a launch of its own
+constexpr int WHOLE_PAGES = 32;     // tables up to this width: a workgroup has whole units, nothing is joined
 
-__device__ inline float xor16_max(float x) { return fmaxf(x, __shfl_xor(x, 16)); }
-__device__ inline float xor32_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
+// over the four lanes that hold a row: lanes 16 apart
+__device__ inline float row_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float row_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
 
 // values that are the same in all lanes, in scalar registers
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -34,11 +50,6 @@ __device__ inline int64_t uniform(int64_t x) {
 struct Range {
   int lo, n;
 };
-
-// What a workgroup leaves about the unit that goes across the border behind its share, if it began in it:
-// shares that have some of it (0: there is none), whether it is not the first unit in its first
-// share, first token, tile, kv head, rows.
-constexpr int BORDER_INTS = 8;
 
 __device__ inline Range request_pages(int kv, int fresh, int window, int width) {
   Range g = {0, 1};
@@ -140,6 +151,16 @@ __device__ inline uint32_t unpack_v(uint32_t w, uint32_t scales) {
   return KvType<DT>::template unpack<I>(w, kv_scale<I>(scales));
 }
 
+// Four tokens of channels c (low nibbles, to lo) and c + 16 (to hi).
+template <int DT>
+__device__ inline void unpack_tokens(uint32_t w, uint32_t sc, u32x4 &lo, u32x4 &hi, int half) {
+  const uint32_t a = unpack_v<DT, 0>(w, sc), b = unpack_v<DT, 1>(w, sc), c = unpack_v<DT, 2>(w, sc), d = unpack_v<DT, 3>(w, sc);
+  lo[half * 2] = __builtin_amdgcn_perm(b, a, 0x05040100);
+  hi[half * 2] = __builtin_amdgcn_perm(b, a, 0x07060302);
+  lo[half * 2 + 1] = __builtin_amdgcn_perm(d, c, 0x05040100);
+  hi[half * 2 + 1] = __builtin_amdgcn_perm(d, c, 0x07060302);
+}
+
 template <int D, int DT>
 __device__ inline void page_values(const Page<D> &pg, const u32x4 *pf, f32x4 *o) {
 #pragma unroll
@@ -148,40 +169,30 @@ __device__ inline void page_values(const Page<D> &pg, const u32x4 *pf, f32x4 *o)
     for (int u = 0; u < 2; ++u) {
       u32x4 lo, hi;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const uint32_t w = pg.v[p][u * 2 + half], sc = pg.vs[p][u * 2 + half];
-        const uint32_t a = unpack_v<DT, 0>(w, sc), b = unpack_v<DT, 1>(w, sc), c = unpack_v<DT, 2>(w, sc),
-                       d = unpack_v<DT, 3>(w, sc);
-        lo[half * 2] = __builtin_amdgcn_perm(b, a, 0x05040100);
-        hi[half * 2] = __builtin_amdgcn_perm(b, a, 0x07060302);
-        lo[half * 2 + 1] = __builtin_amdgcn_perm(d, c, 0x05040100);
-        hi[half * 2 + 1] = __builtin_amdgcn_perm(d, c, 0x07060302);
-      }
+      for (int half = 0; half < 2; ++half) unpack_tokens<DT>(pg.v[p][u * 2 + half], pg.vs[p][u * 2 + half], lo, hi, half);
       o[2 * p] = KvType<DT>::mfma(lo, pf[u], o[2 * p]);
       o[2 * p + 1] = KvType<DT>::mfma(hi, pf[u], o[2 * p + 1]);
     }
 }
 
-// One page into the rows.  first: position of the page's first key; the row sees (low, high].
+// Products of a page with 16 rows into weights, and the rows' state with them.  first: position of the page's first key;
+// the row sees (low, high].  Scores are compared unscaled (scale2 > 0): one multiply-add per exponential.
 template <int D, int DT>
-__device__ inline void page_step(const Page<D> &pg, const u32x4 *qf, Row<D> &r, int lane, float scale2, bool masked,
-                                 int first, int low, int high) {
-  f32x4 s[4];
-  page_scores<D, DT>(pg, qf, lane, s);
-  float top = -__builtin_inff();
+__device__ inline void page_weights(f32x4 *s, Row<D> &r, u32x4 *pf, int g, float scale2, bool masked, int first, int low,
+                                    int high) {
+  if (masked) {
 #pragma unroll
-  for (int tt = 0; tt < 4; ++tt)
+    for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s[tt][i] *= scale2;
-      if (masked) {
-        const int j = first + tt * 16 + (lane >> 4) * 4 + i;
+      for (int i = 0; i < 4; ++i) {
+        const int j = first + tt * 16 + g * 4 + i;
         s[tt][i] = j > low && j <= high ? s[tt][i] : -__builtin_inff();
       }
-      top = fmaxf(top, s[tt][i]);
-    }
-  top = xor32_max(xor16_max(top));
-  const float m = fmaxf(r.m, top);
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e >> 2][e & 3]);
+  const float m = fmaxf(r.m, row_max(top) * scale2);
   if (__any(m > r.m)) {
     const float f = m > r.m ? __builtin_amdgcn_exp2f(r.m - m) : 1.0f;
     r.l *= f;
@@ -192,18 +203,25 @@ __device__ inline void page_step(const Page<D> &pg, const u32x4 *qf, Row<D> &r, 
     r.m = m;
   }
   const float base = m == -__builtin_inff() ? 0.0f : m;  // a row that saw nothing so far: every weight is 0
-  u32x4 pf[2];
 #pragma unroll
   for (int tt = 0; tt < 4; ++tt) {
     float e[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      e[i] = __builtin_amdgcn_exp2f(s[tt][i] - base);
-      r.l += e[i];
-    }
+    for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tt][i], scale2, -base));
+    r.l += (e[0] + e[1]) + (e[2] + e[3]);
     pf[tt >> 1][(tt & 1) * 2] = KvType<DT>::pack(e[0], e[1]);
     pf[tt >> 1][(tt & 1) * 2 + 1] = KvType<DT>::pack(e[2], e[3]);
   }
+}
+
+// One page into 16 rows.
+template <int D, int DT>
+__device__ inline void page_step(const Page<D> &pg, const u32x4 *qf, Row<D> &r, int lane, float scale2, bool masked,
+                                 int first, int low, int high) {
+  f32x4 s[4];
+  u32x4 pf[2];
+  page_scores<D, DT>(pg, qf, lane, s);
+  page_weights<D, DT>(s, r, pf, lane >> 4, scale2, masked, first, low, high);
   page_values<D, DT>(pg, pf, r.o);
 }
 
@@ -212,15 +230,195 @@ __device__ inline void store_row(uint16_t *to, const float *x, int n) {
   for (int c = 0; c < n; c += 2) *reinterpret_cast<uint32_t *>(to + c) = KvType<DT>::pack(x[c], x[c + 1]);
 }
 
-// Rows of a unit: row i of tile `tile` of a group is token i / G, head i % G (of the kv head); with
-// selected pages a group is one token.
+// Rows of a unit: row i of tile `tile` (TR rows each) of a group is token i / G, head i % G (of the kv head); a group
+// is a request or, with selected pages, a token.
 struct Unit {
-  int g, head, tile, lo, pages;  // group, kv head, tile of 16 rows, first page (or list entry), pages
-  int t0, fresh, kv, req;        // first token, tokens, held, request
-  int64_t first;                 // index of its first page among all units' pages
+  int head, tile, lo, pages;         // kv head, tile, first page (or 0: entries of a list), pages
+  int t0, fresh, kv, req, pos0;      // first token, tokens, held, request (-1: none), position of the first token
+  int64_t first;                     // index of its first page among all units' pages
 };
 
-template <int D, int DT, bool SEL>
+// What the workgroups know of each request: units before it and what it takes to place its rows.
+struct Requests {
+  int64_t *prefix;            // [requests]
+  int32_t *t0, *kv, *pos0;    // in LDS, or null: read from the step's arrays
+};
+
+// Whole units are counted instead of their pages.
+template <int TR>
+__device__ inline int64_t units_of(const KvAttnArgs &a, int fresh, int kv) {
+  if (fresh <= 0) return 0;
+  const int64_t n = (((int64_t)fresh * a.group + TR - 1) / TR) * a.kv_heads;
+  return a.whole ? n : n * request_pages(kv, fresh, a.window, a.width).n;
+}
+
+// Units before every request, by the whole workgroup; returns their sum.
+template <int TR, int THREADS>
+__device__ inline int64_t scan_units(const KvAttnArgs &a, const Requests &q, int64_t *sums, int tid) {
+  const int lane = tid & 63, wave = tid >> 6;
+  int64_t carry = 0;
+  for (int b = 0; b < a.requests; b += THREADS) {
+    const int r = b + tid;
+    int64_t n = 0;
+    if (r < a.requests) {
+      const int t0 = a.q_start[r], fresh = min(a.q_start[r + 1], a.tokens) - t0, kv = a.kv_lens[r];
+      n = units_of<TR>(a, fresh, kv);
+      if (q.t0) {
+        q.t0[r] = t0;
+        q.kv[r] = kv;
+        q.pos0[r] = fresh > 0 ? a.positions[t0] : 0;
+        if (r == a.requests - 1) q.t0[r + 1] = t0 + fresh;
+      }
+    }
+    int64_t x = n;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t y = __shfl_up(x, d);
+      if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = x;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) x += sums[w];
+    if (r < a.requests) q.prefix[r] = carry + x - n;
+    for (int w = 0; w < THREADS / 64; ++w) carry += sums[w];
+  }
+  __syncthreads();
+  return uniform(carry);
+}
+
+__global__ __launch_bounds__(1024) void kv_scan_kernel(KvAttnArgs a, int tile_rows) {
+  __shared__ int64_t sums[16];
+  const Requests q = {a.prefix, nullptr, nullptr, nullptr};
+  const int64_t total = tile_rows == 16 ? scan_units<16, 1024>(a, q, sums, threadIdx.x)
+                      : tile_rows == 128 ? scan_units<128, 1024>(a, q, sums, threadIdx.x)
+                                         : scan_units<256, 1024>(a, q, sums, threadIdx.x);
+  if (threadIdx.x == 0) a.prefix[a.requests] = total;
+}
+
+// The unit that index `at` belongs to, and which of its pages that is.
+template <int TR, bool SEL>
+__device__ inline Unit unit_at(const KvAttnArgs &a, const Requests &q, int64_t at, int &offset) {
+  Unit u;
+  int64_t k;  // unit of its group
+  if constexpr (SEL) {
+    const int tiles = (a.group + TR - 1) / TR, n = a.whole ? 1 : a.n_select;
+    const int64_t per = (int64_t)a.kv_heads * tiles * n;
+    u.t0 = (int)(at / per);
+    const int64_t rest = at % per;
+    k = rest / n;
+    offset = (int)(rest % n);
+    u.head = (int)(k / tiles), u.tile = (int)(k % tiles);
+    u.lo = 0, u.pages = a.n_select, u.fresh = 1;
+    const int r = uniform(a.token_req[u.t0]);
+    u.pos0 = uniform(a.positions[u.t0]);
+    u.req = (uint32_t)r < (uint32_t)a.requests ? r : -1;
+    u.kv = u.req >= 0 ? uniform(a.kv_lens[u.req]) : 0;
+  } else {
+    int lo = 0, hi = a.requests;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (uniform(q.prefix[mid]) <= at) lo = mid;
+      else hi = mid;
+    }
+    u.req = lo;
+    if (q.t0) {
+      u.t0 = uniform(q.t0[lo]);
+      u.fresh = uniform(q.t0[lo + 1]) - u.t0;
+      u.kv = uniform(q.kv[lo]);
+      u.pos0 = uniform(q.pos0[lo]);
+    } else {
+      u.t0 = uniform(a.q_start[lo]);
+      u.fresh = min(uniform(a.q_start[lo + 1]), a.tokens) - u.t0;
+      u.kv = uniform(a.kv_lens[lo]);
+      u.pos0 = uniform(a.positions[u.t0]);
+    }
+    const Range pr = request_pages(u.kv, u.fresh, a.window, a.width);
+    const int tiles = (int)(((int64_t)u.fresh * a.group + TR - 1) / TR), n = a.whole ? 1 : pr.n;
+    const int64_t rest = at - uniform(q.prefix[lo]);
+    k = rest / n;
+    offset = (int)(rest % n);
+    u.head = (int)(k / tiles), u.tile = (int)(k % tiles);
+    u.lo = pr.lo, u.pages = pr.n;
+  }
+  u.first = at - offset;
+  return u;
+}
+
+// A workgroup's share: [begin, end) of all units' pages, or whole units.
+struct Share {
+  int64_t total, span, begin, end;
+};
+
+__device__ inline Share share_of(const KvAttnArgs &a, int64_t total, int64_t wg) {
+  Share s;
+  s.total = total;
+  s.span = a.whole ? 1 : (total + a.n_wg - 1) / a.n_wg;
+  if (!a.whole && s.span < 4) s.span = 4;
+  s.begin = wg * s.span;
+  s.end = min(s.begin + s.span, total);
+  return s;
+}
+
+// What a workgroup leaves about the unit that goes across the border behind its share, if it began in it:
+// shares that have some of it (0: there is none), whether it is not the first unit in its first
+// share, first token, tile, kv head, rows.
+constexpr int BORDER_INTS = 8;
+
+__device__ inline void leave_border(const KvAttnArgs &a, const Share &s, const Unit &u, int64_t wg, int64_t at, int rows) {
+  const bool across = u.first + u.pages > s.end && u.first >= s.begin;
+  int32_t *b = a.borders + wg * BORDER_INTS;
+  b[0] = across ? (int32_t)((u.first + u.pages - 1) / s.span - wg) + 1 : 0;
+  b[1] = at != s.begin;
+  b[2] = u.t0;
+  b[3] = u.tile;
+  b[4] = u.head;
+  b[5] = rows;
+}
+
+// The row that a lane works on, and which keys the rows of its 16 see: the row itself (low, high]; every row those in
+// (clear_low, clear_high]; none those outside (any_low, any_high].
+struct Place {
+  int64_t t;
+  int hq, low, high, clear_low, clear_high, any_low, any_high;
+};
+
+template <int TR>
+__device__ inline Place place_of(const KvAttnArgs &a, const Unit &u, int rows, int in_tile) {
+  Place p;
+  const int i = u.tile * TR + min(in_tile, rows - 1);
+  p.t = u.t0 + i / a.group;
+  p.hq = u.head * a.group + i % a.group;
+  // the lane's 16 rows are in order of tokens: their first and last decide
+  const int i0 = u.tile * TR + min(in_tile & ~15, rows - 1), i1 = u.tile * TR + min(in_tile | 15, rows - 1);
+  const int pos = u.pos0 + i / a.group, pos_a = u.pos0 + i0 / a.group, pos_b = u.pos0 + i1 / a.group;
+  p.high = min(pos, u.kv - 1);
+  p.low = a.window > 0 ? pos - a.window : -1;
+  p.clear_high = uniform(min(pos_a, u.kv - 1));
+  p.any_high = uniform(min(pos_b, u.kv - 1));
+  p.clear_low = uniform(a.window > 0 ? pos_b - a.window : -1);
+  p.any_low = uniform(a.window > 0 ? pos_a - a.window : -1);
+  return p;
+}
+
+// A lane's part of its row as the second operand of K Q^T: channels g D/4 + 8 c + 0 .. 7.
+template <int D>
+__device__ inline void load_row(const KvAttnArgs &a, const Place &p, int g, u32x4 *qf) {
+  const uint16_t *at = a.q + p.t * a.q_token + p.hq * a.q_head + g * (D / 4);
+  const uint32_t flip = a.negative ? 0x80008000u : 0u;  // a negative scale: of the row's values
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    qf[c] = *reinterpret_cast<const u32x4 *>(at + c * 8);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) qf[c][j] ^= flip;
+  }
+}
+
+__device__ inline float lse_of(float m, float l) {
+  return l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+
+// A unit's rows from the four wavefronts that had some of its pages each: to the result, or to the workspace.
+template <int D, int DT>
 __device__ inline void join_waves(const KvAttnArgs &a, const Unit &u, int rows, bool whole, int64_t slot, float (*ml)[16][2],
                                   float *buf, int tid) {
   // buf [4][16][D + 4], ml [4]
@@ -250,9 +448,7 @@ __device__ inline void join_waves(const KvAttnArgs &a, const Unit &u, int rows, 
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) x[c] *= inv;
       store_row<DT>(a.out + t * a.out_token + hq * a.out_head + part * (D / 16), x, D / 16);
-      if (a.lse && part == 0)
-        a.lse[t * (a.kv_heads * a.group) + hq] =
-            l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+      if (a.lse && part == 0) a.lse[t * (a.kv_heads * a.group) + hq] = lse_of(m, l);
     }
   } else {
     float *to = a.part_o + (slot * 16 + row) * D + part * (D / 16);
@@ -266,13 +462,13 @@ __device__ inline void join_waves(const KvAttnArgs &a, const Unit &u, int rows, 
 }
 
 // rows that stand for no token: behind the last request's tokens
-template <int D>
+template <int D, int THREADS>
 __device__ inline void clear_rest(const KvAttnArgs &a, int64_t wg, int64_t n_wg, int tid) {
   const int heads = a.kv_heads * a.group;
   int64_t t = a.requests > 0 ? a.q_start[a.requests] : 0;
   if (t < 0) t = 0;
   const int64_t n = (a.tokens - t) * heads;
-  for (int64_t i = wg * 256 + tid; i < n * (D / 8); i += n_wg * 256) {
+  for (int64_t i = wg * THREADS + tid; i < n * (D / 8); i += n_wg * THREADS) {
     const int64_t row = i / (D / 8);
     *reinterpret_cast<u32x4 *>(a.out + (t + row / heads) * a.out_token + (row % heads) * a.out_head + (i % (D / 8)) * 8) =
         u32x4{0, 0, 0, 0};
@@ -280,83 +476,10 @@ __device__ inline void clear_rest(const KvAttnArgs &a, int64_t wg, int64_t n_wg,
   }
 }
 
-// Which group a unit of pages belongs to.  Dense: groups are requests and `prefix` holds the units
-// before each; selected: every token has the same number.
-template <bool SEL>
-__device__ inline Unit unit_at(const KvAttnArgs &a, const int64_t *prefix, int64_t at, int64_t &offset) {
-  Unit u;
-  if constexpr (SEL) {
-    const int tiles = (a.group + 15) / 16;
-    const int64_t per = (int64_t)a.kv_heads * tiles * a.n_select;
-    u.g = (int)(at / per);
-    const int64_t rest = at % per, k = rest / a.n_select;
-    u.head = (int)(k / tiles), u.tile = (int)(k % tiles);
-    u.lo = 0, u.pages = a.n_select;
-    offset = rest % a.n_select;
-    u.t0 = u.g, u.fresh = 1;
-    const int r = uniform(a.token_req[u.g]);
-    u.req = (uint32_t)r < (uint32_t)a.requests ? r : -1;
-    u.kv = u.req >= 0 ? uniform(a.kv_lens[u.req]) : 0;
-  } else {
-    int lo = 0, hi = a.requests;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (uniform(prefix[mid]) <= at) lo = mid;
-      else hi = mid;
-    }
-    u.g = u.req = lo;
-    u.t0 = uniform(a.q_start[lo]);
-    u.fresh = min(uniform(a.q_start[lo + 1]), a.tokens) - u.t0;
-    u.kv = uniform(a.kv_lens[lo]);
-    const Range pr = request_pages(u.kv, u.fresh, a.window, a.width);
-    const int tiles = (int)(((int64_t)u.fresh * a.group + 15) / 16);
-    const int64_t rest = at - uniform(prefix[lo]), k = rest / pr.n;
-    u.head = (int)(k / tiles), u.tile = (int)(k % tiles);
-    u.lo = pr.lo, u.pages = pr.n;
-    offset = rest % pr.n;
-  }
-  u.first = at - offset;
-  return u;
-}
-
-__device__ inline int64_t units_of(const KvAttnArgs &a, int g) {
-  const int fresh = min(a.q_start[g + 1], a.tokens) - a.q_start[g];
-  if (fresh <= 0) return 0;
-  return (((int64_t)fresh * a.group + 15) / 16) * a.kv_heads * request_pages(a.kv_lens[g], fresh, a.window, a.width).n;
-}
-
-// Units before every group, by the whole workgroup; returns their sum.
-__device__ inline int64_t scan_units(const KvAttnArgs &a, int64_t *prefix, int64_t *sums, int tid) {
-  const int lane = tid & 63, wave = tid >> 6;
-  int64_t carry = 0;
-  for (int b = 0; b < a.requests; b += 256) {
-    const int64_t n = b + tid < a.requests ? units_of(a, b + tid) : 0;
-    int64_t x = n;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up(x, d);
-      if (lane >= d) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) sums[wave] = x;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) x += sums[w];
-    if (b + tid < a.requests) prefix[b + tid] = carry + x - n;
-    carry += sums[0] + sums[1] + sums[2] + sums[3];
-  }
-  __syncthreads();
-  return carry;
-}
-
-__global__ __launch_bounds__(256) void kv_scan_kernel(KvAttnArgs a) {
-  __shared__ int64_t sums[4];
-  const int64_t total = scan_units(a, a.prefix, sums, threadIdx.x);
-  if (threadIdx.x == 0) a.prefix[a.requests] = total;
-}
-
-// A workgroup has an equal share of all (group, head, tile, page) units, in this order: ragged
+// A workgroup has an equal share of all (request or token, head, tile, page) units, in this order: ragged
 // requests cost no balance.  Its four wavefronts take the share's pages in turn, each with its own
 // softmax state; what a workgroup has of a unit whose pages it does not have all goes to the
-// workspace, and kv_join_kernel adds up.
+// workspace, and kv_join_kernel adds up.  Where the table is narrow a workgroup has a whole unit instead.
 // Bound by reading the pages (decode: 16 rows or fewer share a page).
 template <int D, int DT, bool SEL>
 __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
@@ -364,69 +487,52 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
   float *buf = reinterpret_cast<float *>(lds);                                     // [4][16][D + 4]
   float(*ml)[16][2] = reinterpret_cast<float(*)[16][2]>(buf + 4 * 16 * (D + 4));  // [4]
   int64_t *sums = reinterpret_cast<int64_t *>(ml + 4);                            // [4]
-  int64_t *own_prefix = sums + 4;                                                 // [requests], dense
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4;
   const int64_t wg = blockIdx.x;
 
-  clear_rest<D>(a, wg, gridDim.x, tid);
+  Requests q = {a.prefix, nullptr, nullptr, nullptr};
   int64_t total;
-  if constexpr (SEL) total = (int64_t)(a.requests > 0 ? min(a.q_start[a.requests], a.tokens) : 0) * a.kv_heads * ((a.group + 15) / 16) * a.n_select;
-  else total = a.scanned ? a.prefix[a.requests] : scan_units(a, own_prefix, sums, tid);
-  const int64_t *prefix = !SEL && a.scanned ? a.prefix : own_prefix;
-  total = uniform(total);
-  int64_t span = (total + a.n_wg - 1) / a.n_wg;
-  if (span < 4) span = 4;
-  const int64_t begin = wg * span, end = min(begin + span, total);
-  if (tid == 0 && begin >= end) a.borders[wg * BORDER_INTS] = 0;
-  for (int64_t at = begin; at < end;) {
-    int64_t offset;
-    const Unit u = unit_at<SEL>(a, prefix, at, offset);
-    const int n = (int)min((int64_t)u.pages - offset, end - at);
+  if constexpr (SEL) {
+    const int tokens = a.requests > 0 ? min(a.q_start[a.requests], a.tokens) : 0;
+    total = (int64_t)tokens * a.kv_heads * ((a.group + 15) / 16) * (a.whole ? 1 : a.n_select);
+  } else if (a.scanned) {
+    total = uniform(a.prefix[a.requests]);
+  } else {
+    q.prefix = sums + 4;                                            // [requests], and [requests + 1] each:
+    q.t0 = reinterpret_cast<int32_t *>(q.prefix + a.requests);
+    q.kv = q.t0 + a.requests + 1;
+    q.pos0 = q.kv + a.requests + 1;
+    total = scan_units<16, 256>(a, q, sums, tid);
+  }
+  const Share share = share_of(a, total, wg);
+  if (tid == 0 && !a.whole && share.begin >= share.end) a.borders[wg * BORDER_INTS] = 0;
+  for (int64_t at = share.begin; at < share.end;) {
+    int offset;
+    const Unit u = unit_at<16, SEL>(a, q, at, offset);
+    const int n = a.whole ? u.pages : (int)min((int64_t)u.pages - offset, share.end - at);
     const int rows = min(16, u.fresh * a.group - u.tile * 16);
-    // the lane's row
-    const int i = u.tile * 16 + min(lane & 15, rows - 1);
-    const int64_t t = u.t0 + i / a.group;
-    const int hq = u.head * a.group + i % a.group;
-    const int pos = a.positions[t];
-    const int high = min(pos, u.kv - 1), low = a.window > 0 ? pos - a.window : -1;
-    // over the wavefront: keys below `clear_high` and above `clear_low` are seen by every row
-    int clear_high = high, clear_low = low, any_high = high, any_low = low;
-    for (int d = 1; d < 16; d <<= 1) {
-      clear_high = min(clear_high, __shfl_xor(clear_high, d));
-      any_high = max(any_high, __shfl_xor(any_high, d));
-      clear_low = max(clear_low, __shfl_xor(clear_low, d));
-      any_low = min(any_low, __shfl_xor(any_low, d));
-    }
-    clear_high = uniform(clear_high);
-    clear_low = uniform(clear_low);
-    any_high = uniform(any_high);
-    any_low = uniform(any_low);
+    const Place p = place_of<16>(a, u, rows, lane & 15);
+    const int32_t *table = a.table + (int64_t)max(u.req, 0) * a.width;
+    const int32_t *list = SEL ? a.selected + ((int64_t)u.t0 * a.kv_heads + u.head) * a.n_select : nullptr;
+    const char *heads = a.pages + u.head * (int64_t)kv_head_bytes(D);
+    const int64_t page_bytes = a.kv_heads * (int64_t)kv_head_bytes(D);
     u32x4 qf[D / 32];
-    {
-      const uint16_t *qp = a.q + t * a.q_token + hq * a.q_head + g * (D / 4);
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) qf[c] = *reinterpret_cast<const u32x4 *>(qp + c * 8);
-    }
+    load_row<D>(a, p, g, qf);
     Row<D> r;
     r.m = -__builtin_inff();
     r.l = 0.0f;
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct) r.o[ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    const int32_t *table = a.table + (int64_t)max(u.req, 0) * a.width;
-    const int32_t *list = SEL ? a.selected + ((int64_t)u.t0 * a.kv_heads + u.head) * a.n_select : nullptr;
-    const char *heads = a.pages + u.head * (int64_t)kv_head_bytes(D);
-    const int64_t page_bytes = a.kv_heads * (int64_t)kv_head_bytes(D);
-    const int k1 = (int)offset + n;
+    const int k1 = offset + n;
     // the wavefront's entries offset + wave, + 4, ...: a lane looks 64 of them up at a time
-    for (int k0 = (int)offset + wave; k0 < k1; k0 += 4 * 64) {
+    for (int k0 = offset + wave; k0 < k1; k0 += 4 * 64) {
       const int k = k0 + 4 * lane;
       int c = -1, page = -1;
       if (k < k1 && u.req >= 0) {
         c = u.lo + k;
         if constexpr (SEL) c = list[k];
-        // a column that no row sees anything of, or without a page in the cache
-        if ((uint32_t)c < (uint32_t)a.width && c * KV_PAGE <= any_high && c * KV_PAGE + KV_PAGE - 1 > any_low) page = table[c];
+        // not a column that no row sees anything of, nor one without a page in the cache
+        if ((uint32_t)c < (uint32_t)a.width && c * KV_PAGE <= p.any_high && c * KV_PAGE + KV_PAGE - 1 > p.any_low) page = table[c];
       }
       uint64_t todo = __ballot((uint32_t)page < (uint64_t)a.n_pages);
       auto fetch = [&](Page<D> &pg, uint64_t left) {
@@ -435,8 +541,8 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
       auto step = [&](Page<D> &pg, uint64_t left) {
         const int first = __builtin_amdgcn_readlane(c, __builtin_ctzll(left)) * KV_PAGE;
         if (first + KV_PAGE > u.kv) pg.cut(u.kv - first, lane);
-        const bool masked = first + KV_PAGE - 1 > clear_high || first <= clear_low;
-        page_step<D, DT>(pg, qf, r, lane, a.scale2, masked, first, low, high);
+        const bool masked = first + KV_PAGE - 1 > p.clear_high || first <= p.clear_low;
+        page_step<D, DT>(pg, qf, r, lane, a.scale2, masked, first, p.low, p.high);
       };
       // a page is requested while the one before it is worked on (256 channels: no registers for two)
       if constexpr (D <= 128) {
@@ -459,35 +565,272 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
         }
       }
     }
-    // l of the whole row
-    r.l += __shfl_xor(r.l, 16);
-    r.l += __shfl_xor(r.l, 32);
+    r.l = row_sum(r.l);
     __syncthreads();  // the buffer is free again
     if (g == 0) ml[wave][lane & 15][0] = r.m, ml[wave][lane & 15][1] = r.l;
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct)
       *reinterpret_cast<f32x4 *>(buf + (wave * 16 + (lane & 15)) * (D + 4) + ct * 16 + g * 4) = r.o[ct];
     __syncthreads();
-    join_waves<D, DT, SEL>(a, u, rows, n == u.pages, 2 * wg + (at != begin), ml, buf, tid);
-    if (tid == 0 && at + n == end) {
-      const bool across = u.first + u.pages > end && u.first >= begin;
-      int32_t *b = a.borders + wg * BORDER_INTS;
-      b[0] = across ? (int32_t)((u.first + u.pages - 1) / span - wg) + 1 : 0;
-      b[1] = at != begin;
-      b[2] = u.t0;
-      b[3] = u.tile;
-      b[4] = u.head;
-      b[5] = rows;
-    }
-    at += n;
+    join_waves<D, DT>(a, u, rows, n == u.pages, 2 * wg + (at != share.begin), ml, buf, tid);
+    const int64_t next = at + (a.whole ? 1 : n);
+    if (tid == 0 && !a.whole && next == share.end) leave_border(a, share, u, wg, at, rows);
+    at = next;
   }
+  clear_rest<D, 256>(a, wg, gridDim.x, tid);
+}
+
+// Fragments of an unpacked page in LDS, 64 lanes of 16 bytes each, as the matrix units take them:
+// keys (tt, c) at tt C + c, values (channel tile ct, token half u) at 4 C + 2 ct + u; C = D / 32.
+template <int D>
+constexpr int page_fragments() { return 4 * (D / 32) + 2 * (D / 16); }
+
+// What a wavefront unpacks of a page: its share of the keys' and values' fragments, a job each of two (keys of 96
+// channels: one) fragments.
+template <int D, int DT, int WAVES>
+struct Unpack {
+  static constexpr int C = D / 32, KF = C % 2 ? 1 : 2, KJOBS = 4 * C / KF, VJOBS = 2 * C;
+  static constexpr int KN = (KJOBS + WAVES - 1) / WAVES, VN = (VJOBS + WAVES - 1) / WAVES;
+  uint32_t k[KN][KF], ks[KN];
+  u32x2 v[VN], vs[VN];
+
+  __device__ inline void load(const char *at, int wave, int lane) {
+    const int row = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      const int job = n * WAVES + wave, tt = job / (C / KF), c = job % (C / KF) * KF;
+      if (job < KJOBS) {
+        const uint32_t *p = reinterpret_cast<const uint32_t *>(at + (tt * 16 + row) * (D / 2) + g * (D / 8)) + c;
+        if constexpr (KF == 2) {
+          const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+          k[n][0] = x[0], k[n][1] = x[1];
+        } else {
+          k[n][0] = p[0];
+        }
+        // the scale of channels 8 (C g + c) ..: the fragments of a job are within 32 channels
+        ks[n] = (uint32_t)*reinterpret_cast<const uint8_t *>(at + kv_kscale_at(D) + (row * C + (C * g + c) / 4) * 4 + tt);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < VN; ++n) {
+      const int job = n * WAVES + wave, p = job >> 1, u = job & 1;
+      if (job < VJOBS) {
+        v[n] = *reinterpret_cast<const u32x2 *>(at + kv_v_at(D) + p * 1024 + lane * 16 + u * 8);
+        vs[n] = *reinterpret_cast<const u32x2 *>(at + kv_vscale_at(D) + p * 64 + g * 16 + u * 8);
+      }
+    }
+  }
+
+  // held: tokens of this page; what is behind them must not meet a weight of 0 as an infinity
+  __device__ inline void store(u32x4 *to, int wave, int lane, int held) {
+    const int g = lane >> 4;
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      const int job = n * WAVES + wave, tt = job / (C / KF), c = job % (C / KF) * KF;
+      if (job < KJOBS) {
+        const float sc = __uint_as_float(ks[n] << 23);
+#pragma unroll
+        for (int f = 0; f < KF; ++f) {
+          u32x4 x;
+          x[0] = KvType<DT>::template unpack<0>(k[n][f], sc);
+          x[1] = KvType<DT>::template unpack<1>(k[n][f], sc);
+          x[2] = KvType<DT>::template unpack<2>(k[n][f], sc);
+          x[3] = KvType<DT>::template unpack<3>(k[n][f], sc);
+          to[(tt * C + c + f) * 64 + lane] = x;
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < VN; ++n) {
+      const int job = n * WAVES + wave, p = job >> 1, u = job & 1;
+      if (job < VJOBS) {
+        u32x4 lo, hi;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t sc = vs[n][half];
+          if (held < KV_PAGE) {
+            const int m = min(max(held - (32 * u + 16 * half + 4 * g), 0), 4);
+            const uint32_t keep = m >= 4 ? 0xffffffffu : (1u << (8 * m)) - 1u;
+            sc = (sc & keep) | (0x01010101u & ~keep);
+          }
+          unpack_tokens<DT>(v[n][half], sc, lo, hi, half);
+        }
+        to[(4 * C + 4 * p + u) * 64 + lane] = lo;
+        to[(4 * C + 4 * p + 2 + u) * 64 + lane] = hi;
+      }
+    }
+  }
+};
+
+// Many rows of one kv head: a workgroup unpacks a page into LDS, one ahead of the one worked on (two
+// buffers, a barrier a page), and each of its wavefronts has NQ times 16 rows with their queries, weights
+// and results in registers.  A fragment read from LDS feeds NQ products.  Bound by the matrix units and the
+// exponentials, which run beside each other as long as two wavefronts share a SIMD.
+template <int D, int DT, int WAVES, int NQ>
+__global__ __launch_bounds__(64 * WAVES, 2) void kv_rows_kernel(KvAttnArgs a) {
+  constexpr int TR = WAVES * NQ * 16, C = D / 32, FRAGS = page_fragments<D>(), THREADS = 64 * WAVES;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  u32x4 *frag = reinterpret_cast<u32x4 *>(lds);                              // [2][FRAGS][64]
+  int64_t *sums = reinterpret_cast<int64_t *>(frag + 2 * FRAGS * 64);        // [WAVES]
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4;
+  const int64_t wg = blockIdx.x;
+
+  Requests q = {a.prefix, nullptr, nullptr, nullptr};
+  int64_t total;
+  if (a.scanned) {
+    total = uniform(a.prefix[a.requests]);
+  } else {
+    q.prefix = sums + WAVES;
+    q.t0 = reinterpret_cast<int32_t *>(q.prefix + a.requests);
+    q.kv = q.t0 + a.requests + 1;
+    q.pos0 = q.kv + a.requests + 1;
+    total = scan_units<TR, THREADS>(a, q, sums, tid);
+  }
+  const Share share = share_of(a, total, wg);
+  if (tid == 0 && !a.whole && share.begin >= share.end) a.borders[wg * BORDER_INTS] = 0;
+  for (int64_t at = share.begin; at < share.end;) {
+    int offset;
+    const Unit u = unit_at<TR, false>(a, q, at, offset);
+    const int n = a.whole ? u.pages : (int)min((int64_t)u.pages - offset, share.end - at);
+    const int rows = min(TR, u.fresh * a.group - u.tile * TR);
+    Place p[NQ];
+    u32x4 qf[NQ][C];
+    Row<D> r[NQ];
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) {
+      p[k] = place_of<TR>(a, u, rows, wave * (NQ * 16) + k * 16 + (lane & 15));
+      load_row<D>(a, p[k], g, qf[k]);
+      r[k].m = -__builtin_inff();
+      r[k].l = 0.0f;
+#pragma unroll
+      for (int ct = 0; ct < D / 16; ++ct) r[k].o[ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // pages that some row of the tile sees
+    const int last = u.tile * TR + rows - 1;
+    const int see_high = min(u.pos0 + last / a.group, u.kv - 1);
+    const int see_low = a.window > 0 ? u.pos0 + u.tile * TR / a.group - a.window + 1 : 0;
+    const int c0 = max(u.lo + offset, max(see_low, 0) / KV_PAGE), c1 = min(u.lo + offset + n, (see_high + KV_PAGE) / KV_PAGE);
+    const int32_t *table = a.table + (int64_t)u.req * a.width;
+    const char *heads = a.pages + u.head * (int64_t)kv_head_bytes(D);
+    const int64_t page_bytes = a.kv_heads * (int64_t)kv_head_bytes(D);
+    const bool idle = wave * (NQ * 16) >= rows;  // no row of this wavefront is one
+
+    Unpack<D, DT, WAVES> job;
+    // the columns with a page in the cache, in order: a lane looks one of 64 up at a time
+    int block = c0, numbers = -1;
+    uint64_t todo = 0;
+    auto look = [&]() {
+      numbers = block + lane < c1 ? table[block + lane] : -1;
+      todo = __ballot((uint32_t)numbers < (uint64_t)a.n_pages);
+    };
+    auto next_page = [&](int &c) -> int {
+      while (!todo) {
+        block += 64;
+        if (block >= c1) return -1;
+        look();
+      }
+      const int j = __builtin_ctzll(todo);
+      todo &= todo - 1;
+      c = block + j;
+      return __builtin_amdgcn_readlane(numbers, j);
+    };
+    look();
+    int c = 0, page = next_page(c), cur = 0;
+    __syncthreads();  // the buffers are free again
+    if (page >= 0) {
+      job.load(heads + page * page_bytes, wave, lane);
+      job.store(frag, wave, lane, u.kv - c * KV_PAGE);
+    }
+    __syncthreads();
+    while (page >= 0) {
+      int cn = 0;
+      const int pn = next_page(cn);
+      if (pn >= 0) job.load(heads + pn * page_bytes, wave, lane);
+      const u32x4 *fr = frag + cur * (FRAGS * 64) + lane;
+      const int first = c * KV_PAGE;
+      bool skip[NQ], all = true;
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) {
+        skip[k] = first > p[k].any_high || first + KV_PAGE - 1 <= p[k].any_low;
+        all = all && skip[k];
+      }
+      if (!idle && !all) {
+        f32x4 s[NQ][4];
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+#pragma unroll
+          for (int k = 0; k < NQ; ++k) s[k][tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int cc = 0; cc < C; ++cc) {
+            const u32x4 x = fr[(tt * C + cc) * 64];
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) s[k][tt] = KvType<DT>::mfma(x, qf[k][cc], s[k][tt]);
+          }
+        }
+        u32x4 pf[NQ][2];
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+          const bool masked = first + KV_PAGE - 1 > p[k].clear_high || first <= p[k].clear_low;
+          page_weights<D, DT>(s[k], r[k], pf[k], g, a.scale2, masked, first, p[k].low, p[k].high);
+        }
+#pragma unroll
+        for (int ct = 0; ct < D / 16; ++ct)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const u32x4 x = fr[(4 * C + 2 * ct + h) * 64];
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) r[k].o[ct] = KvType<DT>::mfma(x, pf[k][h], r[k].o[ct]);
+          }
+      }
+      if (pn >= 0) job.store(frag + (cur ^ 1) * (FRAGS * 64), wave, lane, u.kv - cn * KV_PAGE);
+      __syncthreads();
+      cur ^= 1;
+      c = cn;
+      page = pn;
+    }
+
+    const bool whole = n == u.pages;
+    const int64_t slot = 2 * wg + (at != share.begin);
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) {
+      const float l = row_sum(r[k].l);
+      const int in_tile = wave * (NQ * 16) + k * 16 + (lane & 15);
+      if (whole) {
+        if (in_tile < rows) {
+          const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+          uint16_t *to = a.out + p[k].t * a.out_token + p[k].hq * a.out_head + g * 4;
+#pragma unroll
+          for (int ct = 0; ct < D / 16; ++ct) {
+            u32x2 x;
+            x[0] = KvType<DT>::pack(r[k].o[ct][0] * inv, r[k].o[ct][1] * inv);
+            x[1] = KvType<DT>::pack(r[k].o[ct][2] * inv, r[k].o[ct][3] * inv);
+            *reinterpret_cast<u32x2 *>(to + ct * 16) = x;
+          }
+          if (a.lse && g == 0) a.lse[p[k].t * (a.kv_heads * a.group) + p[k].hq] = lse_of(r[k].m, l);
+        }
+      } else {
+        float *to = a.part_o + (slot * TR + in_tile) * D + g * 4;
+#pragma unroll
+        for (int ct = 0; ct < D / 16; ++ct) *reinterpret_cast<f32x4 *>(to + ct * 16) = r[k].o[ct];
+        if (g == 0) {
+          a.part_ml[(slot * TR + in_tile) * 2] = r[k].m;
+          a.part_ml[(slot * TR + in_tile) * 2 + 1] = l;
+        }
+      }
+    }
+    const int64_t next = at + (a.whole ? 1 : n);
+    if (tid == 0 && !a.whole && next == share.end) leave_border(a, share, u, wg, at, rows);
+    at = next;
+  }
+  clear_rest<D, THREADS>(a, wg, gridDim.x, tid);
 }
 
 // Units that several workgroups share.  Workgroup (w, row) adds up one row's parts of the unit that goes across
-// the border behind share w and began in it.  D / 4 lanes have a part each, so that a context that the whole chip shares is joined in
-// a few trips to memory (520 001 tokens, 64 shares a unit: 40 us with a thread a row and 8 channels, now 4).
+// the border behind share w and began in it.  D / 4 lanes have a part each, so that a context that the whole chip
+// shares is joined in a few trips to memory (520 001 tokens, 64 shares a unit: 40 us with a thread a row
+// and 8 channels, now 5).
 template <int D, int DT>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a, int tile_rows) {
   constexpr int LANES = D / 4, PARTS = 256 / LANES;  // 96 channels: 24 lanes, 10 parts, 16 threads idle
   __shared__ float red_m[4];
   __shared__ f32x4 red_o[PARTS][LANES];
@@ -499,7 +842,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   // a workgroup's first unit is in its slot 0
   auto slot = [&](int k) { return 2 * ((int64_t)blockIdx.x + k) + (k == 0 && late); };
   float m = -__builtin_inff();
-  for (int k = tid; k < n; k += 256) m = fmaxf(m, a.part_ml[(slot(k) * 16 + row) * 2]);
+  for (int k = tid; k < n; k += 256) m = fmaxf(m, a.part_ml[(slot(k) * tile_rows + row) * 2]);
   for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
   if ((tid & 63) == 0) red_m[tid >> 6] = m;
   __syncthreads();
@@ -511,7 +854,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   if (part < PARTS) {
 #pragma unroll 4
     for (int k = part; k < n; k += PARTS) {
-      const int64_t at = slot(k) * 16 + row;
+      const int64_t at = slot(k) * tile_rows + row;
       const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - base);
       l += f * a.part_ml[at * 2 + 1];
       x += f * *reinterpret_cast<const f32x4 *>(a.part_o + at * D + lane * 4);
@@ -526,7 +869,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
     x += red_o[p][lane];
     l += red_l[p];
   }
-  const int i = tile * 16 + row;
+  const int i = tile * tile_rows + row;
   const int64_t t = t0 + i / a.group;
   const int hq = head * a.group + i % a.group;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -534,79 +877,110 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
   r[0] = KvType<DT>::pack(x[0] * inv, x[1] * inv);
   r[1] = KvType<DT>::pack(x[2] * inv, x[3] * inv);
   *reinterpret_cast<u32x2 *>(a.out + t * a.out_token + hq * a.out_head + lane * 4) = r;
-  if (a.lse && lane == 0)
-    a.lse[t * (a.kv_heads * a.group) + hq] = l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  if (a.lse && lane == 0) a.lse[t * (a.kv_heads * a.group) + hq] = lse_of(m, l);
 }
 
-template <int D, int DT, bool SEL>
-int attention_of(KvAttnArgs a, hipStream_t s) {
-  a.scanned = !SEL && a.requests > SCAN_REQUESTS;
-  if (a.scanned) {
-    hipLaunchKernelGGL(kv_scan_kernel, dim3(1), dim3(256), 0, s, a);
-    KV_HIP_TRY(hipGetLastError());
-  }
-  const size_t lds = (size_t)(4 * 16 * (D + 4) + 4 * 16 * 2) * 4 + 4 * 8 + (SEL || a.scanned ? 0 : (size_t)a.requests * 8);
-  if (lds > 65536) KV_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&kv_rows16_kernel<D, DT, SEL>),
-                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-  hipLaunchKernelGGL((kv_rows16_kernel<D, DT, SEL>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
-  KV_HIP_TRY(hipGetLastError());
-  if (a.n_wg == 1) return IVFPQ_OK;
-  const int rows = (int)(a.tokens * (int64_t)a.group < 16 ? a.tokens * (int64_t)a.group : !SEL || a.group > 16 ? 16 : a.group);
-  hipLaunchKernelGGL((kv_join_kernel<D, DT>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a);
-  KV_HIP_TRY(hipGetLastError());
-  return IVFPQ_OK;
-}
-
-template <int D>
-int attention_typed(const KvAttnArgs &a, int dtype, hipStream_t s) {
-  if (dtype == IVFPQ_KV_BF16)
-    return a.selected ? attention_of<D, IVFPQ_KV_BF16, true>(a, s) : attention_of<D, IVFPQ_KV_BF16, false>(a, s);
-  return a.selected ? attention_of<D, IVFPQ_KV_FP16, true>(a, s) : attention_of<D, IVFPQ_KV_FP16, false>(a, s);
-}
-
+// How a call is cut: rows of a tile, workgroups, whole units or shares, and the workspace.
 struct Shape {
-  int64_t units;   // (group, head, tile), at most
-  int n_wg;
+  int tile_rows, n_wg;
+  bool whole;
   size_t prefix, borders, ml, o;  // bytes
 };
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int n_select, int64_t width) {
+Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int n_select, int64_t width) {
   Shape s;
-  s.units = n_select > 0 ? tokens * kv_heads * ((group + 15) / 16) : (tokens * group / 16 + requests) * kv_heads;
-  const int64_t pages = s.units * (n_select > 0 ? n_select : width);
-  // two workgroups on every CU, four pages each at least
-  s.n_wg = pages / 4 >= 512 ? 512 : (int)(pages / 4 + 1);
+  const int64_t rows = (int64_t)(max_new < tokens ? max_new : tokens) * group;  // of a request and head, at most
+  const int big = D == 256 ? 128 : 256;
+  s.tile_rows = n_select > 0 || rows <= 64 ? 16 : big;
+  const int64_t units = n_select > 0 ? tokens * kv_heads * ((group + 15) / 16)
+                                     : (tokens * group / s.tile_rows + requests) * kv_heads;
+  const int64_t pages = units * (n_select > 0 ? n_select : width);
+  if (s.tile_rows == 16) {
+    // two workgroups on every CU, four pages each at least
+    s.whole = (n_select > 0 ? n_select : width) <= WHOLE_PAGES;
+    s.n_wg = s.whole ? (int)units : pages / 4 >= 512 ? 512 : (int)(pages / 4 + 1);
+  } else {
+    // one workgroup on every CU; more units than workgroups need no shares
+    s.whole = units >= 1024 || width <= 4;
+    s.n_wg = s.whole ? (int)units : pages / 4 >= 256 ? 256 : (int)(pages / 4 + 1);
+  }
+  if (s.n_wg < 1) s.n_wg = 1;
   s.prefix = up256((size_t)(requests + 1) * 8);
-  s.borders = up256((size_t)s.n_wg * BORDER_INTS * 4);
-  s.ml = up256((size_t)s.n_wg * 2 * 16 * 2 * 4);
-  s.o = up256((size_t)s.n_wg * 2 * 16 * D * 4);
+  s.borders = s.whole ? 0 : up256((size_t)s.n_wg * BORDER_INTS * 4);
+  s.ml = s.whole ? 0 : up256((size_t)s.n_wg * 2 * s.tile_rows * 2 * 4);
+  s.o = s.whole ? 0 : up256((size_t)s.n_wg * 2 * s.tile_rows * D * 4);
   return s;
+}
+
+template <typename K>
+int allow_lds(K kernel, size_t lds) {
+  if (lds > 65536)
+    KV_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+  return IVFPQ_OK;
+}
+
+template <int D, int DT>
+int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
+  const bool sel = a.selected != nullptr;
+  a.scanned = !sel && a.requests > SCAN_REQUESTS;
+  if (a.scanned) {
+    hipLaunchKernelGGL(kv_scan_kernel, dim3(1), dim3(1024), 0, s, a, sh.tile_rows);
+    KV_HIP_TRY(hipGetLastError());
+  }
+  const size_t lists = sel || a.scanned ? 0 : (size_t)a.requests * 8 + 3 * (size_t)(a.requests + 1) * 4;
+  int rc;
+  if (sh.tile_rows == 16) {
+    const size_t lds = (size_t)(4 * 16 * (D + 4) + 4 * 16 * 2) * 4 + 4 * 8 + lists;
+    if (sel) {
+      if ((rc = allow_lds(&kv_rows16_kernel<D, DT, true>, lds))) return rc;
+      hipLaunchKernelGGL((kv_rows16_kernel<D, DT, true>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
+    } else {
+      if ((rc = allow_lds(&kv_rows16_kernel<D, DT, false>, lds))) return rc;
+      hipLaunchKernelGGL((kv_rows16_kernel<D, DT, false>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
+    }
+  } else {
+    constexpr int NQ = D == 256 ? 1 : 2;
+    const size_t lds = (size_t)2 * page_fragments<D>() * 1024 + 8 * 8 + lists;
+    if ((rc = allow_lds(&kv_rows_kernel<D, DT, 8, NQ>, lds))) return rc;
+    hipLaunchKernelGGL((kv_rows_kernel<D, DT, 8, NQ>), dim3((unsigned)a.n_wg), dim3(512), lds, s, a);
+  }
+  KV_HIP_TRY(hipGetLastError());
+  if (a.whole || a.n_wg == 1) return IVFPQ_OK;
+  const int64_t most = a.tokens * (int64_t)a.group;
+  const int rows = (int)(sel && a.group < 16 ? a.group : most < sh.tile_rows ? most : sh.tile_rows);
+  hipLaunchKernelGGL((kv_join_kernel<D, DT>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a, sh.tile_rows);
+  KV_HIP_TRY(hipGetLastError());
+  return IVFPQ_OK;
+}
+
+template <int D>
+int attention_typed(const KvAttnArgs &a, int dtype, const Shape &sh, hipStream_t s) {
+  return dtype == IVFPQ_KV_BF16 ? attention_of<D, IVFPQ_KV_BF16>(a, sh, s) : attention_of<D, IVFPQ_KV_FP16>(a, sh, s);
 }
 
 }  // namespace
 
 size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int n_select,
                               int64_t width) {
-  (void)max_new;
-  const Shape s = shape_of(tokens, requests, kv_heads, group, D, n_select, width);
+  const Shape s = shape_of(tokens, requests, kv_heads, group, D, max_new, n_select, width);
   return s.prefix + s.borders + s.ml + s.o;
 }
 
 int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s) {
-  (void)max_new;
-  const Shape sh = shape_of(a.tokens, a.requests, a.kv_heads, a.group, D, a.selected ? a.n_select : 0, a.width);
+  const Shape sh = shape_of(a.tokens, a.requests, a.kv_heads, a.group, D, max_new, a.selected ? a.n_select : 0, a.width);
   a.n_wg = sh.n_wg;
+  a.whole = sh.whole;
   a.prefix = reinterpret_cast<int64_t *>(workspace);
   a.borders = reinterpret_cast<int32_t *>(workspace + sh.prefix);
   a.part_ml = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders);
   a.part_o = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders + sh.ml);
   switch (D) {
-    case 64: return attention_typed<64>(a, dtype, s);
-    case 96: return attention_typed<96>(a, dtype, s);
-    case 128: return attention_typed<128>(a, dtype, s);
-    default: return attention_typed<256>(a, dtype, s);
+    case 64: return attention_typed<64>(a, dtype, sh, s);
+    case 96: return attention_typed<96>(a, dtype, sh, s);
+    case 128: return attention_typed<128>(a, dtype, sh, s);
+    default: return attention_typed<256>(a, dtype, sh, s);
   }
 }
 

@@ -59,13 +59,14 @@ struct KvAttnArgs {
   const int32_t *table, *q_start, *kv_lens, *token_req, *positions, *selected;
   int64_t q_token, q_head, out_token, out_head, n_pages;
   int32_t kv_heads, group, requests, tokens, width, n_select, window;
-  float scale2;  // scale * log2(e)
-  // split over pages: workgroup w takes [w, w + 1) * span of the (group, head, tile, page) units in order
-  int32_t n_wg, scanned;
+  float scale2;  // |scale| log2(e), above 0
+  int32_t negative;  // the scale was below 0
+  // workgroups; whether each has a whole unit of rows instead of a share of all units' pages; whether prefix is filled
+  int32_t n_wg, whole, scanned;
   int64_t *prefix;   // [requests + 1]: units before each request, where a launch of its own scans them
   int32_t *borders;  // [n_wg][8]: the unit that goes on in the next share
-  float *part_ml;   // [2 n_wg][rows][2]
-  float *part_o;    // [2 n_wg][rows][D]
+  float *part_ml;    // [2 n_wg][rows of a tile][2]: parts of units that go across borders
+  float *part_o;     // [2 n_wg][rows of a tile][D]
 };
 
 int launch_kv_plan(const KvPlanArgs &a, hipStream_t s);

@@ -338,6 +338,23 @@ def test_attention_chunks(kv, dtype, H, G, D):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("H,G,D", SHAPES)
+def test_attention_shares_across_requests(kv, dtype, H, G, D):
+    """Tables wide enough that workgroups have shares of all requests' pages: shares that begin and end inside requests,
+    heads and tiles, requests of one page between long ones, some without new tokens."""
+    rng = np.random.default_rng(D * G + 1)
+    s = Server(kv, rng, dtype, H, D, 150, 6, 50)
+    s.fill([0, 2900, 5, 64, 1300, 700])
+    s.fill([1, 1, 0, 1, 1, 1], max_tokens=7)
+    s.attend(H * G, max_new=1)
+    s.attend(H * G, max_new=1, window=700)
+    s.fill([70, 33, 0, 129, 1, 5], max_tokens=240)
+    s.attend(H * G)
+    s.attend(H * G, window=300)
+    s.attend(H * G, max_new=1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_attention_long_context_is_split(kv, dtype):
     """One request long enough that many workgroups share its pages."""
     rng = np.random.default_rng(31)
