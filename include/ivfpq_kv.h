@@ -142,6 +142,8 @@ typedef struct {
   float *lse;              /* device [max_tokens][heads], or NULL                             */
 } ivfpq_kv_attention_args;
 
+/* Bytes for a call with these arguments (rows, strides and pointers of `args` are not looked at).  What is asked for
+ * without a window is enough with one. */
 size_t ivfpq_kv_attention_workspace_bytes(const ivfpq_kv_cache *cache, const ivfpq_kv_step *step,
                                           const ivfpq_kv_attention_args *args);
 int ivfpq_kv_attention(const ivfpq_kv_cache *cache, const ivfpq_kv_step *step, const ivfpq_kv_attention_args *args,

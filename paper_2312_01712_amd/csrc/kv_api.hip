@@ -105,6 +105,7 @@ int check_attention(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, const ivfpq
     set_error("%s: n_select = %d outside [0, %d]", fn, a->n_select, IVFPQ_KV_MAX_SELECT);
     return IVFPQ_ERR_INVALID_ARGUMENT;
   }
+  if (a->window < 0) return invalid(fn, "window must be >= 0");
   if (a->max_new < 1 && s->max_tokens > 0) return invalid(fn, "max_new must be positive");
   // the launch's grid has a workgroup per token, kv head and 16 heads of a group
   const int64_t group = a->heads / c->kv_heads;
@@ -219,7 +220,7 @@ int ivfpq_kv_select(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, ivfpq_kv_ro
 size_t ivfpq_kv_attention_workspace_bytes(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, const ivfpq_kv_attention_args *a) {
   if (check_attention(c, s, a, "kv_attention_workspace_bytes")) return 0;
   return kv_attention_workspace(s->max_tokens, s->requests, c->kv_heads, a->heads / c->kv_heads, c->head_dim, a->max_new,
-                                a->n_select, s->table_width);
+                                a->window, a->n_select, s->table_width);
 }
 
 int ivfpq_kv_attention(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, const ivfpq_kv_attention_args *x, void *d_workspace,
@@ -228,7 +229,6 @@ int ivfpq_kv_attention(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, const iv
   int rc = check_attention(c, s, x, fn);
   if (rc) return rc;
   if (!isfinite(x->scale)) return invalid(fn, "scale must be finite");
-  if (x->window < 0) return invalid(fn, "window must be >= 0");
   if (s->max_tokens == 0) return IVFPQ_OK;
   if ((x->selected != nullptr) != (x->n_select > 0)) return invalid(fn, "selected and n_select go together");
   rc = check_step_arrays(s, fn);
@@ -240,7 +240,7 @@ int ivfpq_kv_attention(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, const iv
   const int group = x->heads / c->kv_heads;
   rc = check_workspace(d_workspace, workspace_bytes,
                        kv_attention_workspace(s->max_tokens, s->requests, c->kv_heads, group, c->head_dim, x->max_new,
-                                              x->n_select, s->table_width), fn);
+                                              x->window, x->n_select, s->table_width), fn);
   if (rc) return rc;
   KvAttnArgs a = {};
   a.pages = static_cast<const char *>(c->pages); a.q = static_cast<const uint16_t *>(x->q.data);

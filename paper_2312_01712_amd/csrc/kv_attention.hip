@@ -825,49 +825,58 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv_rows_kernel(KvAttnArgs a) {
   clear_rest<D, THREADS>(a, wg, gridDim.x, tid);
 }
 
-// Units that several workgroups share.  Workgroup (w, row) adds up one row's parts of the unit that goes across
-// the border behind share w and began in it.  D / 4 lanes have a part each, so that a context that the whole chip
-// shares is joined in a few trips to memory (520 001 tokens, 64 shares a unit: 40 us with a thread a row
-// and 8 channels, now 5).
-template <int D, int DT>
+// Units that several workgroups share.  Workgroup (w, y) adds up the parts of ROWS rows of the unit that goes across
+// the border behind share w and began in it.  D / 4 lanes have a part (ROWS = 1) or a row each: decode has one
+// tile of few rows and up to all shares in a unit (520 001 tokens, 64 shares a unit: 40 us with a thread a row
+// and 8 channels, now 5), chunks have many rows of few parts (a workgroup a row there: 29 us for 256 shares).
+template <int D, int DT, bool ONE>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a, int tile_rows) {
-  constexpr int LANES = D / 4, PARTS = 256 / LANES;  // 96 channels: 24 lanes, 10 parts, 16 threads idle
+  constexpr int LANES = D / 4, SETS = 256 / LANES;  // 96 channels: 24 lanes, 10 sets, 16 threads idle
   __shared__ float red_m[4];
-  __shared__ f32x4 red_o[PARTS][LANES];
-  __shared__ float red_l[PARTS];
-  const int tid = threadIdx.x, row = blockIdx.y;
+  __shared__ f32x4 red_o[ONE ? SETS : 1][LANES];
+  __shared__ float red_l[SETS];
+  const int tid = threadIdx.x, set = tid / LANES, lane = tid % LANES;
+  const int row = ONE ? blockIdx.y : blockIdx.y * SETS + set;
   const int32_t *b = a.borders + (int64_t)blockIdx.x * BORDER_INTS;
   const int n = b[0], late = b[1], t0 = b[2], tile = b[3], head = b[4], rows = b[5];
-  if (n == 0 || row >= rows) return;
+  if (n == 0 || (ONE ? row : (int)blockIdx.y * SETS) >= rows) return;
   // a workgroup's first unit is in its slot 0
   auto slot = [&](int k) { return 2 * ((int64_t)blockIdx.x + k) + (k == 0 && late); };
-  float m = -__builtin_inff();
-  for (int k = tid; k < n; k += 256) m = fmaxf(m, a.part_ml[(slot(k) * tile_rows + row) * 2]);
-  for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  if ((tid & 63) == 0) red_m[tid >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
-  const float base = m == -__builtin_inff() ? 0.0f : m;
-  const int part = tid / LANES, lane = tid % LANES;
+  float m = -__builtin_inff(), l = 0.0f;
   f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-  float l = 0.0f;
-  if (part < PARTS) {
+  if constexpr (ONE) {
+    for (int k = tid; k < n; k += 256) m = fmaxf(m, a.part_ml[(slot(k) * tile_rows + row) * 2]);
+    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if ((tid & 63) == 0) red_m[tid >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+  } else {
+    if (set >= SETS || row >= rows) return;
 #pragma unroll 4
-    for (int k = part; k < n; k += PARTS) {
+    for (int k = 0; k < n; ++k) m = fmaxf(m, a.part_ml[(slot(k) * tile_rows + row) * 2]);
+  }
+  const float base = m == -__builtin_inff() ? 0.0f : m;
+  if (set < SETS) {
+#pragma unroll 4
+    for (int k = ONE ? set : 0; k < n; k += ONE ? SETS : 1) {
       const int64_t at = slot(k) * tile_rows + row;
       const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - base);
       l += f * a.part_ml[at * 2 + 1];
       x += f * *reinterpret_cast<const f32x4 *>(a.part_o + at * D + lane * 4);
     }
-    red_o[part][lane] = x;
-    if (lane == 0) red_l[part] = l;
   }
-  __syncthreads();
-  if (part > 0) return;
+  if constexpr (ONE) {
+    if (set < SETS) {
+      red_o[set][lane] = x;
+      if (lane == 0) red_l[set] = l;
+    }
+    __syncthreads();
+    if (set > 0) return;
 #pragma unroll
-  for (int p = 1; p < PARTS; ++p) {
-    x += red_o[p][lane];
-    l += red_l[p];
+    for (int p = 1; p < SETS; ++p) {
+      x += red_o[p][lane];
+      l += red_l[p];
+    }
   }
   const int i = tile * tile_rows + row;
   const int64_t t = t0 + i / a.group;
@@ -889,23 +898,25 @@ struct Shape {
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int n_select, int64_t width) {
+Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int window, int n_select,
+               int64_t width) {
   Shape s;
   const int64_t rows = (int64_t)(max_new < tokens ? max_new : tokens) * group;  // of a request and head, at most
-  const int big = D == 256 ? 128 : 256;
-  s.tile_rows = n_select > 0 || rows <= 64 ? 16 : big;
+  // tiles of 256 rows where they fill the CUs (a page is unpacked by twice the wavefronts: a chunk of 2048 tokens,
+  // 32 heads, behind 8190: 449 us for 483 with 128), of 128 otherwise; 256 channels have no registers for more
+  s.tile_rows = n_select > 0 || rows <= 64 ? 16 : D < 256 && tokens * group * kv_heads >= 256 * 256 ? 256 : 128;
   const int64_t units = n_select > 0 ? tokens * kv_heads * ((group + 15) / 16)
                                      : (tokens * group / s.tile_rows + requests) * kv_heads;
-  const int64_t pages = units * (n_select > 0 ? n_select : width);
-  if (s.tile_rows == 16) {
-    // two workgroups on every CU, four pages each at least
-    s.whole = (n_select > 0 ? n_select : width) <= WHOLE_PAGES;
-    s.n_wg = s.whole ? (int)units : pages / 4 >= 512 ? 512 : (int)(pages / 4 + 1);
-  } else {
-    // one workgroup on every CU; more units than workgroups need no shares
-    s.whole = units >= 1024 || width <= 4;
-    s.n_wg = s.whole ? (int)units : pages / 4 >= 256 ? 256 : (int)(pages / 4 + 1);
+  int64_t most = n_select > 0 ? n_select : width;  // pages of a unit
+  if (n_select == 0 && window > 0) {
+    const int64_t seen = ((int64_t)window + (max_new < tokens ? max_new : tokens)) / KV_PAGE + 2;
+    if (seen < most) most = seen;
   }
+  // whole units where they are short, or (chunks) where there are many; shares otherwise: as many workgroups as the
+  // chip holds at a time, four pages each at least
+  const int fill = s.tile_rows == 16 ? 512 : s.tile_rows == 128 && D < 256 ? 512 : 256;
+  s.whole = most <= WHOLE_PAGES || (s.tile_rows > 16 && units >= 1024);
+  s.n_wg = s.whole ? (int)units : units * most / 4 >= fill ? fill : (int)(units * most / 4 + 1);
   if (s.n_wg < 1) s.n_wg = 1;
   s.prefix = up256((size_t)(requests + 1) * 8);
   s.borders = s.whole ? 0 : up256((size_t)s.n_wg * BORDER_INTS * 4);
@@ -941,16 +952,29 @@ int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
       hipLaunchKernelGGL((kv_rows16_kernel<D, DT, false>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
     }
   } else {
-    constexpr int NQ = D == 256 ? 1 : 2;
     const size_t lds = (size_t)2 * page_fragments<D>() * 1024 + 8 * 8 + lists;
-    if ((rc = allow_lds(&kv_rows_kernel<D, DT, 8, NQ>, lds))) return rc;
-    hipLaunchKernelGGL((kv_rows_kernel<D, DT, 8, NQ>), dim3((unsigned)a.n_wg), dim3(512), lds, s, a);
+    if constexpr (D == 256) {
+      if ((rc = allow_lds(&kv_rows_kernel<D, DT, 8, 1>, lds))) return rc;
+      hipLaunchKernelGGL((kv_rows_kernel<D, DT, 8, 1>), dim3((unsigned)a.n_wg), dim3(512), lds, s, a);
+    } else if (sh.tile_rows == 256) {
+      if ((rc = allow_lds(&kv_rows_kernel<D, DT, 8, 2>, lds))) return rc;
+      hipLaunchKernelGGL((kv_rows_kernel<D, DT, 8, 2>), dim3((unsigned)a.n_wg), dim3(512), lds, s, a);
+    } else {
+      if ((rc = allow_lds(&kv_rows_kernel<D, DT, 4, 2>, lds))) return rc;
+      hipLaunchKernelGGL((kv_rows_kernel<D, DT, 4, 2>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
+    }
   }
   KV_HIP_TRY(hipGetLastError());
   if (a.whole || a.n_wg == 1) return IVFPQ_OK;
   const int64_t most = a.tokens * (int64_t)a.group;
-  const int rows = (int)(sel && a.group < 16 ? a.group : most < sh.tile_rows ? most : sh.tile_rows);
-  hipLaunchKernelGGL((kv_join_kernel<D, DT>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a, sh.tile_rows);
+  if (sh.tile_rows == 16) {
+    const int rows = (int)(sel && a.group < 16 ? a.group : most < 16 ? most : 16);
+    hipLaunchKernelGGL((kv_join_kernel<D, DT, true>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a, 16);
+  } else {
+    constexpr int SETS = 256 / (D / 4);
+    hipLaunchKernelGGL((kv_join_kernel<D, DT, false>), dim3((unsigned)(a.n_wg - 1), (unsigned)((sh.tile_rows + SETS - 1) / SETS)),
+                       dim3(256), 0, s, a, sh.tile_rows);
+  }
   KV_HIP_TRY(hipGetLastError());
   return IVFPQ_OK;
 }
@@ -962,14 +986,15 @@ int attention_typed(const KvAttnArgs &a, int dtype, const Shape &sh, hipStream_t
 
 }  // namespace
 
-size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int n_select,
-                              int64_t width) {
-  const Shape s = shape_of(tokens, requests, kv_heads, group, D, max_new, n_select, width);
+size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int window,
+                              int n_select, int64_t width) {
+  const Shape s = shape_of(tokens, requests, kv_heads, group, D, max_new, window, n_select, width);
   return s.prefix + s.borders + s.ml + s.o;
 }
 
 int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s) {
-  const Shape sh = shape_of(a.tokens, a.requests, a.kv_heads, a.group, D, max_new, a.selected ? a.n_select : 0, a.width);
+  const Shape sh = shape_of(a.tokens, a.requests, a.kv_heads, a.group, D, max_new, a.window, a.selected ? a.n_select : 0,
+                            a.width);
   a.n_wg = sh.n_wg;
   a.whole = sh.whole;
   a.prefix = reinterpret_cast<int64_t *>(workspace);

@@ -72,8 +72,8 @@ struct KvAttnArgs {
 int launch_kv_plan(const KvPlanArgs &a, hipStream_t s);
 int launch_kv_append(const KvAppendArgs &a, int D, int dtype, hipStream_t s);
 int launch_kv_select(const KvSelectArgs &a, int D, int dtype, hipStream_t s);
-size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int n_select,
-                              int64_t width);
+size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_new, int window,
+                              int n_select, int64_t width);
 int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s);
 
 #define KV_HIP_TRY(expr)                                \
