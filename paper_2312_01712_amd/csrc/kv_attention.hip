@@ -662,6 +662,13 @@ struct Unpack {
   }
 };
 
+// A barrier that orders the workgroup's LDS accesses and leaves loads from memory on their way.
+__device__ inline void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Many rows of one kv head: a workgroup unpacks a page into LDS, one ahead of the one worked on (two
 // buffers, a barrier a page), and each of its wavefronts has NQ times 16 rows with their queries, weights
 // and results in registers.  A fragment read from LDS feeds NQ products.  Bound by the matrix units and the
@@ -735,17 +742,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv_rows_kernel(KvAttnArgs a) {
       return __builtin_amdgcn_readlane(numbers, j);
     };
     look();
+    // the page worked on is in LDS, the next in registers, requested a page's work ago
     int c = 0, page = next_page(c), cur = 0;
-    __syncthreads();  // the buffers are free again
+    int cn = 0, pn = -1;
+    lds_barrier();  // the buffers are free again
     if (page >= 0) {
       job.load(heads + page * page_bytes, wave, lane);
       job.store(frag, wave, lane, u.kv - c * KV_PAGE);
-    }
-    __syncthreads();
-    while (page >= 0) {
-      int cn = 0;
-      const int pn = next_page(cn);
+      pn = next_page(cn);
       if (pn >= 0) job.load(heads + pn * page_bytes, wave, lane);
+    }
+    lds_barrier();
+    while (page >= 0) {
       const u32x4 *fr = frag + cur * (FRAGS * 64) + lane;
       const int first = c * KV_PAGE;
       bool skip[NQ], all = true;
@@ -782,11 +790,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv_rows_kernel(KvAttnArgs a) {
             for (int k = 0; k < NQ; ++k) r[k].o[ct] = KvType<DT>::mfma(x, pf[k][h], r[k].o[ct]);
           }
       }
-      if (pn >= 0) job.store(frag + (cur ^ 1) * (FRAGS * 64), wave, lane, u.kv - cn * KV_PAGE);
-      __syncthreads();
-      cur ^= 1;
-      c = cn;
       page = pn;
+      c = cn;
+      if (pn >= 0) {
+        job.store(frag + (cur ^ 1) * (FRAGS * 64), wave, lane, u.kv - cn * KV_PAGE);
+        pn = next_page(cn);
+        if (pn >= 0) job.load(heads + pn * page_bytes, wave, lane);
+      }
+      lds_barrier();
+      cur ^= 1;
     }
 
     const bool whole = n == u.pages;
