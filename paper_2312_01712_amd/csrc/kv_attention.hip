@@ -175,11 +175,10 @@ __device__ inline void page_values(const Page<D> &pg, const u32x4 *pf, f32x4 *o)
     }
 }
 
-// Products of a page with 16 rows into weights, and the rows' state with them.  first: position of the page's first key;
-// the row sees (low, high].  Scores are compared unscaled (scale2 > 0): one multiply-add per exponential.
-template <int D, int DT>
-__device__ inline void page_weights(f32x4 *s, Row<D> &r, u32x4 *pf, int g, float scale2, bool masked, int first, int low,
-                                    int high) {
+// The largest product of a page joins a row's maximum; what the row has so far shrinks with it.  first: position of the
+// page's first key; the row sees (low, high].  Products are compared unscaled (scale2 > 0): one multiply-add an exponential.
+template <int D>
+__device__ inline void page_maximum(f32x4 *s, Row<D> &r, int g, float scale2, bool masked, int first, int low, int high) {
   if (masked) {
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
@@ -202,7 +201,12 @@ __device__ inline void page_weights(f32x4 *s, Row<D> &r, u32x4 *pf, int g, float
       for (int i = 0; i < 4; ++i) r.o[ct][i] *= f;
     r.m = m;
   }
-  const float base = m == -__builtin_inff() ? 0.0f : m;  // a row that saw nothing so far: every weight is 0
+}
+
+// Products into weights, as the second operand of V^T P^T, and their sum.
+template <int D, int DT>
+__device__ inline void page_weights(const f32x4 *s, Row<D> &r, u32x4 *pf, float scale2) {
+  const float base = r.m == -__builtin_inff() ? 0.0f : r.m;  // a row that saw nothing so far: every weight is 0
 #pragma unroll
   for (int tt = 0; tt < 4; ++tt) {
     float e[4];
@@ -221,7 +225,8 @@ __device__ inline void page_step(const Page<D> &pg, const u32x4 *qf, Row<D> &r, 
   f32x4 s[4];
   u32x4 pf[2];
   page_scores<D, DT>(pg, qf, lane, s);
-  page_weights<D, DT>(s, r, pf, lane >> 4, scale2, masked, first, low, high);
+  page_maximum<D>(s, r, lane >> 4, scale2, masked, first, low, high);
+  page_weights<D, DT>(s, r, pf, scale2);
   page_values<D, DT>(pg, pf, r.o);
 }
 
@@ -674,7 +679,7 @@ __device__ inline void lds_barrier() {
 // and results in registers.  A fragment read from LDS feeds NQ products.  Bound by the matrix units and the
 // exponentials, which run beside each other as long as two wavefronts share a SIMD.
 template <int D, int DT, int WAVES, int NQ>
-__global__ __launch_bounds__(64 * WAVES, 2) void kv_rows_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv_rows_kernel(KvAttnArgs a) {
   constexpr int TR = WAVES * NQ * 16, C = D / 32, FRAGS = page_fragments<D>(), THREADS = 64 * WAVES;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   u32x4 *frag = reinterpret_cast<u32x4 *>(lds);                              // [2][FRAGS][64]
@@ -763,32 +768,49 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv_rows_kernel(KvAttnArgs a) {
         all = all && skip[k];
       }
       if (!idle && !all) {
+        // four fragments are on their way from LDS while the products of the four before them run
+        u32x4 x[2][4];
+        auto read = [&](int f, u32x4 *to) {
+#pragma unroll
+          for (int b = 0; b < 4; ++b) to[b] = fr[(f + b) * 64];
+        };
         f32x4 s[NQ][4];
 #pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
+        for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
           for (int k = 0; k < NQ; ++k) s[k][tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        read(0, x[0]);
 #pragma unroll
-          for (int cc = 0; cc < C; ++cc) {
-            const u32x4 x = fr[(tt * C + cc) * 64];
+        for (int f = 0; f < 4 * C; f += 4) {
+          if (f + 4 < 4 * C) read(f + 4, x[(f / 4 + 1) & 1]);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int k = 0; k < NQ; ++k) s[k][tt] = KvType<DT>::mfma(x, qf[k][cc], s[k][tt]);
-          }
+          for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) s[k][(f + b) / C] = KvType<DT>::mfma(x[(f / 4) & 1][b], qf[k][(f + b) % C], s[k][(f + b) / C]);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        u32x4 pf[NQ][2];
 #pragma unroll
         for (int k = 0; k < NQ; ++k) {
           const bool masked = first + KV_PAGE - 1 > p[k].clear_high || first <= p[k].clear_low;
-          page_weights<D, DT>(s[k], r[k], pf[k], g, a.scale2, masked, first, p[k].low, p[k].high);
+          page_maximum<D>(s[k], r[k], g, a.scale2, masked, first, p[k].low, p[k].high);
         }
+        read(4 * C, x[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        u32x4 pf[NQ][2];
 #pragma unroll
-        for (int ct = 0; ct < D / 16; ++ct)
+        for (int k = 0; k < NQ; ++k) page_weights<D, DT>(s[k], r[k], pf[k], a.scale2);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const u32x4 x = fr[(4 * C + 2 * ct + h) * 64];
+        for (int f = 0; f < D / 8; f += 4) {
+          if (f + 4 < D / 8) read(4 * C + f + 4, x[(f / 4 + 1) & 1]);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int k = 0; k < NQ; ++k) r[k].o[ct] = KvType<DT>::mfma(x, pf[k][h], r[k].o[ct]);
-          }
+          for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int k = 0; k < NQ; ++k)
+              r[k].o[(f + b) >> 1] = KvType<DT>::mfma(x[(f / 4) & 1][b], pf[k][b & 1], r[k].o[(f + b) >> 1]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
       page = pn;
       c = cn;
