@@ -62,38 +62,37 @@ typedef struct {
 /* Bytes of one page, all kv heads; 0 where head_dim or kv_heads is not supported. */
 size_t ivfpq_kv_page_bytes(int32_t kv_heads, int32_t head_dim);
 
-/* One step as the plan leaves it; all arrays on the device.  Tokens are the step's new tokens,
- * request by request; rows max_tokens - q_start[requests] at the end stand for no token. */
+/* One step; all arrays on the device.  Tokens are the step's new tokens, request by request; rows
+ * max_tokens - q_start[requests] at the end stand for no token. */
 typedef struct {
-  int32_t requests;         /* 0 .. IVFPQ_KV_MAX_REQUESTS                                */
-  int32_t max_tokens;       /* rows of the per-token arrays                              */
-  int32_t table_width;      /* pages that a row of the table has room for, 1 .. 2^20     */
-  const int32_t *kv_lens;   /* [requests]      tokens held, the new ones among them      */
-  const int32_t *q_start;   /* [requests + 1]  first new token of a request              */
-  const int32_t *table;     /* [requests][table_width] page numbers                      */
-  const int64_t *slots;     /* [max_tokens]    page * 64 + place in the page, or -1      */
-  const int32_t *token_req; /* [max_tokens]    request, or -1                            */
-  const int32_t *positions; /* [max_tokens]    position in the request, or -1            */
+  int32_t requests;    /* 0 .. IVFPQ_KV_MAX_REQUESTS                                         */
+  int32_t max_tokens;  /* rows of the per-token arrays                                       */
+  int32_t table_width; /* pages that a row of the table has room for, 1 .. 2^20              */
+  int32_t *table;      /* [requests][table_width] page numbers; the caller's, kept over steps */
+  int32_t *kv_lens;    /* the rest is written by ivfpq_kv_plan and read by the other calls:
+                          [requests]      tokens held, the new ones among them               */
+  int32_t *q_start;    /* [requests + 1]  first new token of a request                       */
+  int64_t *slots;      /* [max_tokens]    page * 64 + place in the page, or -1               */
+  int32_t *token_req;  /* [max_tokens]    request, or -1                                     */
+  int32_t *positions;  /* [max_tokens]    position in the request, or -1                     */
 } ivfpq_kv_step;
 
 /* Page tables and slot maps of a step.
  *   past_lens   [requests]  tokens held (a negative one counts as 0)
  *   new_lens    [requests]  new tokens; negative: the request ends, its pages go back
- *   table       [requests][table_width], entries below ceil(past / 64) are the pages held; written
- *               from there to ceil((past + new) / 64), -1 where no page was left
+ *   step->table entries below ceil(past / 64) are the pages held; written from there to
+ *               ceil((past + new) / 64), -1 where no page was left
  *   free_pages  [free_capacity] ring of the pages that nobody holds; free_state [3]: first taken
  *               index, first index behind them (both count up), and how many pages were missing.
  *               Pages are taken in the order of requests and positions, those of ended requests
  *               are put behind the others and can be taken from the next step on.
  *               free_state_out must not be free_state.
  * Written: table and free_pages in place (doing a step again from the same lengths and state
- * gives the same), kv_lens (0 for an ended request), q_start, slots, token_req, positions and
- * free_state_out.  A step has to fit: past + new <= 64 * table_width (what is beyond has slot -1 and is
- * not counted as held), and the sum of new <= max_tokens.  requests == 0 marks all rows as no token. */
-int ivfpq_kv_plan(int32_t requests, const int32_t *past_lens, const int32_t *new_lens, int32_t *table,
-                  int32_t table_width, int32_t *free_pages, int64_t free_capacity, const int64_t *free_state,
-                  int64_t *free_state_out, int32_t *kv_lens, int32_t *q_start, int64_t *slots, int32_t *token_req,
-                  int32_t *positions, int32_t max_tokens, void *hip_stream);
+ * gives the same), the step's other arrays (kv_lens: 0 for an ended request) and free_state_out.  A step has to
+ * fit: past + new <= 64 * table_width (what is beyond has slot -1 and is not counted as held), and the
+ * sum of new <= max_tokens.  kv_lens must not be past_lens.  requests == 0 marks all rows as no token. */
+int ivfpq_kv_plan(const ivfpq_kv_step *step, const int32_t *past_lens, const int32_t *new_lens, int32_t *free_pages,
+                  int64_t free_capacity, const int64_t *free_state, int64_t *free_state_out, void *hip_stream);
 
 /* Rows [tokens][heads][head_dim] of the cache's type, the channels contiguous; base 16-byte
  * aligned, strides in elements, multiples of 8 (a stride that no index uses is not looked at). */

@@ -127,28 +127,26 @@ size_t ivfpq_kv_page_bytes(int32_t kv_heads, int32_t head_dim) {
   return (size_t)kv_heads * kv_head_bytes(head_dim);
 }
 
-int ivfpq_kv_plan(int32_t requests, const int32_t *past_lens, const int32_t *new_lens, int32_t *table,
-                  int32_t table_width, int32_t *free_pages, int64_t free_capacity, const int64_t *free_state,
-                  int64_t *free_state_out, int32_t *kv_lens, int32_t *q_start, int64_t *slots, int32_t *token_req,
-                  int32_t *positions, int32_t max_tokens, void *stream) {
+int ivfpq_kv_plan(const ivfpq_kv_step *s, const int32_t *past_lens, const int32_t *new_lens, int32_t *free_pages,
+                  int64_t free_capacity, const int64_t *free_state, int64_t *free_state_out, void *stream) {
   const char *fn = "kv_plan";
-  ivfpq_kv_step s = {requests, max_tokens, table_width, kv_lens, q_start, table, slots, token_req, positions};
-  int rc = check_step(&s, fn);
+  int rc = check_step(s, fn);
   if (rc) return rc;
-  rc = check_step_arrays(&s, fn);
+  rc = check_step_arrays(s, fn);
   if (rc) return rc;
-  if (!q_start || (requests > 0 && (!past_lens || !new_lens)) || (max_tokens > 0 && !slots)) return invalid(fn, "NULL array");
+  if (!s->q_start || (s->requests > 0 && (!past_lens || !new_lens)) || (s->max_tokens > 0 && !s->slots)) return invalid(fn, "NULL array");
   if (!free_pages || !free_state || !free_state_out) return invalid(fn, "NULL ring of free pages");
   if (free_state == free_state_out) return invalid(fn, "free_state_out must not be free_state");
+  if (s->requests > 0 && (s->kv_lens == past_lens || s->kv_lens == new_lens)) return invalid(fn, "kv_lens must not be past_lens or new_lens");
   if (free_capacity < 1 || free_capacity > ((int64_t)1 << 25)) {
     set_error("%s: free_capacity = %lld outside [1, 2^25]", fn, (long long)free_capacity);
     return IVFPQ_ERR_INVALID_ARGUMENT;
   }
   KvPlanArgs a = {};
-  a.past = past_lens; a.fresh = new_lens; a.table = table; a.free_pages = free_pages; a.kv_lens = kv_lens;
-  a.q_start = q_start; a.token_req = token_req; a.positions = positions; a.slots = slots; a.state = free_state;
-  a.state_out = free_state_out; a.capacity = free_capacity; a.requests = requests; a.width = table_width;
-  a.max_tokens = max_tokens;
+  a.past = past_lens; a.fresh = new_lens; a.table = s->table; a.free_pages = free_pages; a.kv_lens = s->kv_lens;
+  a.q_start = s->q_start; a.token_req = s->token_req; a.positions = s->positions; a.slots = s->slots; a.state = free_state;
+  a.state_out = free_state_out; a.capacity = free_capacity; a.requests = s->requests; a.width = s->table_width;
+  a.max_tokens = s->max_tokens;
   return launch_kv_plan(a, static_cast<hipStream_t>(stream));
 }
 

@@ -17,7 +17,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from .binding import IvfpqError, _check, _dev, _stream, load_library  # noqa: F401
+from .binding import IvfpqError, _check, _dev, load_library  # noqa: F401
 
 PAGE = 64
 MAX_REQUESTS, MAX_SELECT = 65536, 1024
@@ -37,8 +37,8 @@ class _Cache(ctypes.Structure):
 
 
 class _Step(ctypes.Structure):
-    _fields_ = [("requests", _i32), ("max_tokens", _i32), ("table_width", _i32), ("kv_lens", _vp), ("q_start", _vp),
-                ("table", _vp), ("slots", _vp), ("token_req", _vp), ("positions", _vp)]
+    _fields_ = [("requests", _i32), ("max_tokens", _i32), ("table_width", _i32), ("table", _vp), ("kv_lens", _vp),
+                ("q_start", _vp), ("slots", _vp), ("token_req", _vp), ("positions", _vp)]
 
 
 class _Rows(ctypes.Structure):
@@ -61,7 +61,7 @@ def _lib():
         cp, sp, ap = ctypes.POINTER(_Cache), ctypes.POINTER(_Step), ctypes.POINTER(_Attention)
         lib.ivfpq_kv_page_bytes.argtypes = [_i32, _i32]
         lib.ivfpq_kv_page_bytes.restype = _sz
-        lib.ivfpq_kv_plan.argtypes = [_i32, _vp, _vp, _vp, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp]
+        lib.ivfpq_kv_plan.argtypes = [sp, _vp, _vp, _vp, _i64, _vp, _vp, _vp]
         lib.ivfpq_kv_append.argtypes = [cp, _Rows, _Rows, _vp, _i64, _vp, _vp, _vp]
         lib.ivfpq_kv_select_workspace_bytes.argtypes = [cp, sp, _i32]
         lib.ivfpq_kv_select_workspace_bytes.restype = _sz
@@ -73,20 +73,43 @@ def _lib():
     return _ready
 
 
-def _rows(t: torch.Tensor, dtype, shape, device, what: str) -> _Rows:
+# The checks below run several times in every call of a decode loop, where the host is what
+# costs: one comparison each where everything fits, the full check with its message where it does not.
+
+
+def _ptr(t: torch.Tensor, dtype, shape, device: int, what: str) -> int:
+    """Address of a contiguous tensor of this dtype, shape (None: any extent) and device."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _dev(t, dtype, shape, device, what).data_ptr()
+
+
+def _rows(t: torch.Tensor, dtype, shape, device: int, what: str) -> _Rows:
     """Rows [tokens][heads][head_dim] that the kernels may read or write where they are: any strides
     of tokens and heads that keep rows on 16 bytes, channels contiguous."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype:
         raise ValueError(f"{what}: expected a CUDA tensor of {dtype}, got {getattr(t, 'dtype', type(t))} on "
                          f"{getattr(t, 'device', 'the host')}")
-    if t.device.index != device:
-        raise ValueError(f"{what}: on cuda:{t.device.index}, the cache lives on cuda:{device}")
-    if t.dim() != 3 or any(e is not None and g != e for g, e in zip(t.shape, shape)):
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on {t.device}, the cache lives on cuda:{device}")
+    if t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(t.shape)} does not match {tuple(shape)}")
     ts, hs, cs = t.stride()
     if cs != 1:
         raise ValueError(f"{what}: the channels must be contiguous, their stride is {cs}")
-    return _Rows(t.data_ptr() if t.numel() else None, ts, hs)
+    return _Rows(t.data_ptr() or None, ts, hs)
+
+
+def _heads_of(q: torch.Tensor) -> int:
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q: expected a tensor [tokens][heads][head_dim]")
+    return q.shape[1]
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 class Step:
@@ -109,8 +132,9 @@ class Step:
         _dev(positions, torch.int32, (T,), dev, "positions")
         _dev(free_state, torch.int64, (3,), dev, "free_state")
         self.max_tokens = T
-        self._c = _Step(R, T, table.shape[1], kv_lens.data_ptr(), q_start.data_ptr(), table.data_ptr(), slots.data_ptr(),
+        self._c = _Step(R, T, table.shape[1], table.data_ptr(), kv_lens.data_ptr(), q_start.data_ptr(), slots.data_ptr(),
                         requests.data_ptr(), positions.data_ptr())
+        self._ref, self._state = ctypes.byref(self._c), free_state.data_ptr()
 
     @classmethod
     def empty(cls, requests: int, max_tokens: int, table: torch.Tensor) -> "Step":
@@ -125,24 +149,21 @@ def plan(past_lens: torch.Tensor, new_lens: torch.Tensor, table: torch.Tensor, f
          free_state: torch.Tensor, max_tokens: Optional[int] = None, out: Optional[Step] = None) -> Step:
     """Page tables and slot maps of a step (`ivfpq_kv_plan`).  past_lens, new_lens [R] int32 (new < 0: the request
     ends); table [R][W] and free_pages [capacity] int32 are updated in place; free_state [3] int64."""
-    table = _dev(table, torch.int32, (None, None), what="table")
-    R, dev = table.shape[0], table.device.index
-    _dev(past_lens, torch.int32, (R,), dev, "past_lens")
-    _dev(new_lens, torch.int32, (R,), dev, "new_lens")
-    _dev(free_pages, torch.int32, (None,), dev, "free_pages")
-    _dev(free_state, torch.int64, (3,), dev, "free_state")
     if out is None:
         if max_tokens is None:
             raise ValueError("plan: max_tokens, the most new tokens of the step, is needed without out")
-        out = Step.empty(R, int(max_tokens), table)
-    elif out._c.requests != R or out.table.data_ptr() != table.data_ptr() or out.table.shape != table.shape:
-        raise ValueError("plan: out was made for another table")
+        table = _dev(table, torch.int32, (None, None), what="table")
+        out = Step.empty(table.shape[0], int(max_tokens), table)
     elif max_tokens is not None and max_tokens != out.max_tokens:
         raise ValueError(f"plan: out has {out.max_tokens} rows, max_tokens is {max_tokens}")
-    c = out._c
-    _check(_lib().ivfpq_kv_plan(R, past_lens.data_ptr(), new_lens.data_ptr(), c.table, c.table_width, free_pages.data_ptr(),
-                                free_pages.shape[0], free_state.data_ptr(), out.free_state.data_ptr(), c.kv_lens, c.q_start,
-                                c.slots, c.token_req, c.positions, c.max_tokens, _stream()))
+    c, dev = out._c, out._checked
+    R = c.requests
+    if _ptr(table, torch.int32, (R, c.table_width), dev, "table") != (c.table or 0):
+        raise ValueError("plan: out was made for another table")
+    ring = _ptr(free_pages, torch.int32, free_pages.shape[:1], dev, "free_pages")
+    _check(_lib().ivfpq_kv_plan(out._ref, _ptr(past_lens, torch.int32, (R,), dev, "past_lens"),
+                                _ptr(new_lens, torch.int32, (R,), dev, "new_lens"), ring, free_pages.shape[0],
+                                _ptr(free_state, torch.int64, (3,), dev, "free_state"), out._state, _raw_stream(dev)))
     return out
 
 
@@ -164,6 +185,7 @@ class KvCache:
         self.boxes = torch.zeros(n_pages, kv_heads, 2, head_dim, dtype=torch.bfloat16, device=device)
         self.device = self.pages.device.index
         self._c = _Cache(n_pages, kv_heads, head_dim, _DTYPES[dtype], self.pages.data_ptr(), self.boxes.data_ptr())
+        self._ref = ctypes.byref(self._c)
 
     def free_ring(self) -> Tuple[torch.Tensor, torch.Tensor]:
         """(free_pages, free_state) of a cache whose pages are all free."""
@@ -175,47 +197,44 @@ class KvCache:
                rounded: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> None:
         """Rounds k, v [T][kv_heads][head_dim] into the pages at slots [T] int64; `rounded`: two tensors of that shape
         for the values as they are held."""
-        T = k.shape[0]
-        shape = (T, self.kv_heads, self.head_dim)
-        kr, vr = _rows(k, self.dtype, shape, self.device, "k"), _rows(v, self.dtype, shape, self.device, "v")
-        _dev(slots, torch.int64, (T,), self.device, "slots")
-        to = [None, None]
+        shape = (slots.shape[0], self.kv_heads, self.head_dim)
+        dtype, dev = self.dtype, self.device
+        kr, vr = _rows(k, dtype, shape, dev, "k"), _rows(v, dtype, shape, dev, "v")
+        at = _ptr(slots, torch.int64, shape[:1], dev, "slots")
+        to_k = to_v = None
         if rounded is not None:
-            to = [_dev(t, self.dtype, shape, self.device, "rounded").data_ptr() for t in rounded]
-        _check(_lib().ivfpq_kv_append(ctypes.byref(self._c), kr, vr, slots.data_ptr(), T, to[0], to[1], _stream()))
+            to_k, to_v = _ptr(rounded[0], dtype, shape, dev, "rounded k"), _ptr(rounded[1], dtype, shape, dev, "rounded v")
+        _check(_lib().ivfpq_kv_append(self._ref, kr, vr, at, shape[0], to_k, to_v, _raw_stream(dev)))
 
     def _step(self, step: Step):
         if step._checked != self.device:
             raise ValueError(f"step: on cuda:{step._checked}, the cache lives on cuda:{self.device}")
-        return ctypes.byref(step._c)
+        return step._ref
 
-    def _workspace(self, workspace, need: int) -> torch.Tensor:
-        if workspace is None:
-            return torch.empty(max(need, 1), dtype=torch.uint8, device=self.pages.device)
-        return _dev(workspace, torch.uint8, (None,), self.device, "workspace")
+    def _workspace(self, need: int) -> torch.Tensor:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=self.pages.device)
 
     def select_workspace(self, step: Step, heads: int) -> torch.Tensor:
-        return self._workspace(None, _lib().ivfpq_kv_select_workspace_bytes(ctypes.byref(self._c), self._step(step), heads))
+        return self._workspace(_lib().ivfpq_kv_select_workspace_bytes(self._ref, self._step(step), heads))
 
     def select(self, q: torch.Tensor, step: Step, n_pages: int, sinks: int = 1, recent: int = 1,
                out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The n_pages table columns that each token and kv head looks at, ascending, -1 behind them
         (`ivfpq_kv_select`): [T][kv_heads][n_pages] int32.  q [T][heads][head_dim]."""
-        T = step.max_tokens
-        qr = _rows(q, self.dtype, (T, None, self.head_dim), self.device, "q")
+        T, heads, dev = step.max_tokens, _heads_of(q), self.device
+        qr = _rows(q, self.dtype, (T, heads, self.head_dim), dev, "q")
         if out is None:
             out = torch.empty((T, self.kv_heads, max(n_pages, 0)), dtype=torch.int32, device=q.device)
-        else:
-            _dev(out, torch.int32, (T, self.kv_heads, n_pages), self.device, "out")
-        ws = self.select_workspace(step, q.shape[1]) if workspace is None else self._workspace(workspace, 0)
-        _check(_lib().ivfpq_kv_select(ctypes.byref(self._c), self._step(step), qr, q.shape[1], n_pages, sinks, recent,
-                                      out.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
+        to = _ptr(out, torch.int32, (T, self.kv_heads, max(n_pages, 0)), dev, "out")
+        ws = self.select_workspace(step, heads) if workspace is None else workspace
+        size = ws.shape[0]
+        _check(_lib().ivfpq_kv_select(self._ref, self._step(step), qr, heads, n_pages, sinks, recent, to,
+                                      _ptr(ws, torch.uint8, (size,), dev, "workspace"), size, _raw_stream(dev)))
         return out
 
     def attention_workspace(self, step: Step, heads: int, max_new: Optional[int] = None, n_select: int = 0) -> torch.Tensor:
         args = _Attention(heads=heads, max_new=step.max_tokens if max_new is None else max_new, n_select=n_select)
-        return self._workspace(None, _lib().ivfpq_kv_attention_workspace_bytes(ctypes.byref(self._c), self._step(step),
-                                                                               ctypes.byref(args)))
+        return self._workspace(_lib().ivfpq_kv_attention_workspace_bytes(self._ref, self._step(step), ctypes.byref(args)))
 
     def attention(self, q: torch.Tensor, step: Step, scale: Optional[float] = None, window: int = 0,
                   pages: Optional[torch.Tensor] = None, max_new: Optional[int] = None, out: Optional[torch.Tensor] = None,
@@ -224,28 +243,27 @@ class KvCache:
         q [T][heads][head_dim]; scale: head_dim ** -0.5 unless given; window: tokens seen, the token itself among
         them (0: all); pages: [T][kv_heads][n] int32 from `select`; max_new: no request has more new tokens (a hint
         that decides how the work is cut; T unless given).  Returns (out as q, lse [T][heads] fp32)."""
-        T = step.max_tokens
-        qr = _rows(q, self.dtype, (T, None, self.head_dim), self.device, "q")
-        heads = q.shape[1]
+        T, heads, dev, dtype = step.max_tokens, _heads_of(q), self.device, self.dtype
+        shape = (T, heads, self.head_dim)
+        qr = _rows(q, dtype, shape, dev, "q")
         if out is None:
-            out = torch.empty((T, heads, self.head_dim), dtype=self.dtype, device=q.device)
-        to = _rows(out, self.dtype, (T, heads, self.head_dim), self.device, "out")
+            out = torch.empty(shape, dtype=dtype, device=q.device)
+        to = _rows(out, dtype, shape, dev, "out")
         if lse is None:
             lse = torch.empty((T, heads), dtype=torch.float32, device=q.device)
-        else:
-            _dev(lse, torch.float32, (T, heads), self.device, "lse")
-        n_select = 0
+        to_lse = _ptr(lse, torch.float32, (T, heads), dev, "lse")
+        n_select, lists = 0, None
         if pages is not None:
-            _dev(pages, torch.int32, (T, self.kv_heads, None), self.device, "pages")
-            n_select = pages.shape[2]
+            n_select = pages.shape[-1]
+            lists = _ptr(pages, torch.int32, (T, self.kv_heads, n_select), dev, "pages") or None
             if n_select < 1:
                 raise ValueError("pages: at least one page for a token and kv head")
         if max_new is None:
             max_new = max(T, 1)
-        ws = self.attention_workspace(step, heads, max_new, n_select) if workspace is None else self._workspace(workspace, 0)
-        args = _Attention(qr, heads, max_new, self.head_dim ** -0.5 if scale is None else scale, window,
-                          pages.data_ptr() if n_select else None, n_select, to.data, to.token_stride, to.head_stride,
-                          lse.data_ptr())
-        _check(_lib().ivfpq_kv_attention(ctypes.byref(self._c), self._step(step), ctypes.byref(args), ws.data_ptr(),
-                                         ws.numel(), _stream()))
+        ws = self.attention_workspace(step, heads, max_new, n_select) if workspace is None else workspace
+        size = ws.shape[0]
+        args = _Attention(qr, heads, max_new, self.head_dim ** -0.5 if scale is None else scale, window, lists, n_select,
+                          to.data, to.token_stride, to.head_stride, to_lse)
+        _check(_lib().ivfpq_kv_attention(self._ref, self._step(step), ctypes.byref(args),
+                                         _ptr(ws, torch.uint8, (size,), dev, "workspace"), size, _raw_stream(dev)))
         return out, lse

@@ -93,11 +93,14 @@ def test_append_and_plan_refuse():
     assert lib.ivfpq_kv_append(c, rows(), rows(), P, 3, P + 2, None, None) == BAD
     assert lib.ivfpq_kv_append(None, rows(), rows(), P, 3, None, None, None) == BAD
     assert lib.ivfpq_kv_append(c, rows(None), rows(None), None, 0, None, None, None) == binding.OK
-    args = dict(requests=2, past=P, new=P, table=P, width=4, ring=P, capacity=8, state=P, state_out=P + 64, kv_lens=P, q_start=P,
-                slots=P, token_req=P, positions=P, max_tokens=3)
-    for over in (dict(requests=-1), dict(past=None), dict(table=None), dict(ring=None), dict(capacity=0), dict(state=None),
-                 dict(state_out=P), dict(q_start=None), dict(slots=None), dict(width=0), dict(max_tokens=-1)):
-        assert lib.ivfpq_kv_plan(*{**args, **over}.values(), None) == BAD, over
+    args = dict(past=P, new=P, ring=P, capacity=8, state=P, state_out=P + 64)
+    def plan(over_step={}, **over):
+        return lib.ivfpq_kv_plan(ctypes.byref(step(kv_lens=P + 64, **over_step)), *{**args, **over}.values(), None)
+    for over in (dict(requests=-1), dict(table=None), dict(q_start=None), dict(slots=None), dict(table_width=0), dict(max_tokens=-1)):
+        assert plan(over) == BAD, over
+    for over in (dict(past=None), dict(ring=None), dict(capacity=0), dict(state=None), dict(state_out=P), dict(past=P + 64)):
+        assert plan(**over) == BAD, over
+    assert lib.ivfpq_kv_plan(None, *args.values(), None) == BAD
     assert lib.ivfpq_kv_select_workspace_bytes(None, None, 1) == 0
     assert lib.ivfpq_kv_attention_workspace_bytes(None, None, None) == 0
     assert lib.ivfpq_kv_page_bytes(8, 128) == 8 * 68 * 128 and lib.ivfpq_kv_page_bytes(8, 100) == 0 and lib.ivfpq_kv_page_bytes(0, 64) == 0
