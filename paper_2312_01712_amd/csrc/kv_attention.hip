@@ -295,6 +295,7 @@ __global__ __launch_bounds__(1024) void kv_scan_kernel(KvAttnArgs a, int tile_ro
   __shared__ int64_t sums[16];
   const Requests q = {a.prefix, nullptr, nullptr, nullptr};
   const int64_t total = tile_rows == 16 ? scan_units<16, 1024>(a, q, sums, threadIdx.x)
+                      : tile_rows == 64 ? scan_units<64, 1024>(a, q, sums, threadIdx.x)
                       : tile_rows == 128 ? scan_units<128, 1024>(a, q, sums, threadIdx.x)
                                          : scan_units<256, 1024>(a, q, sums, threadIdx.x);
   if (threadIdx.x == 0) a.prefix[a.requests] = total;
@@ -679,7 +680,7 @@ __device__ inline void lds_barrier() {
 // and results in registers.  A fragment read from LDS feeds NQ products.  Bound by the matrix units and the
 // exponentials, which run beside each other as long as two wavefronts share a SIMD.
 template <int D, int DT, int WAVES, int NQ>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void kv_rows_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, WAVES * NQ == 4 ? 3 : 2))) void kv_rows_kernel(KvAttnArgs a) {
   constexpr int TR = WAVES * NQ * 16, C = D / 32, FRAGS = page_fragments<D>(), THREADS = 64 * WAVES;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   u32x4 *frag = reinterpret_cast<u32x4 *>(lds);                              // [2][FRAGS][64]
@@ -936,20 +937,24 @@ Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D,
                int64_t width) {
   Shape s;
   const int64_t rows = (int64_t)(max_new < tokens ? max_new : tokens) * group;  // of a request and head, at most
-  // tiles of 256 rows where they fill the CUs (a page is unpacked by twice the wavefronts: a chunk of 2048 tokens,
-  // 32 heads, behind 8190: 449 us for 483 with 128), of 128 otherwise; 256 channels have no registers for more
-  s.tile_rows = n_select > 0 || rows <= 64 ? 16 : D < 256 && tokens * group * kv_heads >= 256 * 256 ? 256 : 128;
-  const int64_t units = n_select > 0 ? tokens * kv_heads * ((group + 15) / 16)
-                                     : (tokens * group / s.tile_rows + requests) * kv_heads;
   int64_t most = n_select > 0 ? n_select : width;  // pages of a unit
   if (n_select == 0 && window > 0) {
     const int64_t seen = ((int64_t)window + (max_new < tokens ? max_new : tokens)) / KV_PAGE + 2;
     if (seen < most) most = seen;
   }
+  const bool narrow = most <= WHOLE_PAGES;
+  // Chunks: tiles of 256 rows where they fill the CUs (a page is unpacked by twice the wavefronts: 2048 tokens,
+  // 32 heads, behind 8190: 349 us, 128 rows 380), of 128 otherwise, and of 64 where units are short, so that shares
+  // cannot fill the chip instead (1700 tokens, 16 heads of their own keys, a window of 1000: 38 us, 128 rows 44).
+  // 256 channels have no registers for more than 16 rows a wavefront.
+  const int64_t all = tokens * group * kv_heads;
+  s.tile_rows = n_select > 0 || rows <= 64 ? 16 : D == 256 ? 128 : all >= 256 * 256 ? 256 : narrow && all < 512 * 128 ? 64 : 128;
+  const int64_t units = n_select > 0 ? tokens * kv_heads * ((group + 15) / 16)
+                                     : (tokens * group / s.tile_rows + requests) * kv_heads;
   // whole units where they are short, or (chunks) where there are many; shares otherwise: as many workgroups as the
   // chip holds at a time, four pages each at least
   const int fill = s.tile_rows == 16 ? 512 : s.tile_rows == 128 && D < 256 ? 512 : 256;
-  s.whole = most <= WHOLE_PAGES || (s.tile_rows > 16 && units >= 1024);
+  s.whole = narrow || (s.tile_rows > 16 && units >= 1024);
   s.n_wg = s.whole ? (int)units : units * most / 4 >= fill ? fill : (int)(units * most / 4 + 1);
   if (s.n_wg < 1) s.n_wg = 1;
   s.prefix = up256((size_t)(requests + 1) * 8);
@@ -993,6 +998,9 @@ int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
     } else if (sh.tile_rows == 256) {
       if ((rc = allow_lds(&kv_rows_kernel<D, DT, 8, 2>, lds))) return rc;
       hipLaunchKernelGGL((kv_rows_kernel<D, DT, 8, 2>), dim3((unsigned)a.n_wg), dim3(512), lds, s, a);
+    } else if (sh.tile_rows == 64) {
+      if ((rc = allow_lds(&kv_rows_kernel<D, DT, 4, 1>, lds))) return rc;
+      hipLaunchKernelGGL((kv_rows_kernel<D, DT, 4, 1>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
     } else {
       if ((rc = allow_lds(&kv_rows_kernel<D, DT, 4, 2>, lds))) return rc;
       hipLaunchKernelGGL((kv_rows_kernel<D, DT, 4, 2>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
