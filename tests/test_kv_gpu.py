@@ -462,6 +462,26 @@ def test_more_requests_than_are_scanned_in_a_workgroup(kv):
     s.attend(2, max_new=1)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("D,W", [(64, 60), (128, 60), (96, 30)])
+def test_attention_of_many_rows(kv, dtype, D, W):
+    """Enough rows for the largest tiles: prompts of many requests at once, some behind what they hold; odd numbers of
+    pages, pages that are missing in the middle of a request."""
+    rng = np.random.default_rng(D)
+    R = 31
+    s = Server(kv, rng, dtype, 1, D, 420, R, W)
+    s.fill(rng.integers(0, 90, R))
+    new = rng.integers(1, 140, R)
+    new[3], new[4] = 500, 0
+    s.fill(new, max_tokens=int(new.sum()) + 2)
+    assert new.sum() * 32 >= 256 * 256
+    for at in ((3, 1), (3, 4), (8, 0)):  # holes in the tables
+        s.table[at] = -1
+    s.want["table"] = s.table
+    s.d_table.copy_(dev(s.table, torch.int32))
+    s.attend(32)
+
+
 @pytest.mark.parametrize("max_new", [1, 3, 17, 64, 1000])
 def test_the_hint_does_not_change_what_is_computed(kv, max_new):
     """max_new only chooses how the work is cut; below the truth too."""
