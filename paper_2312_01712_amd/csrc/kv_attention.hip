@@ -42,10 +42,6 @@ __device__ inline float row_sum(float x) {
 
 // values that are the same in all lanes, in scalar registers
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ inline int64_t uniform(int64_t x) {
-  return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
-}
-
 // pages [lo, lo + n) that any new token of a request sees; n >= 1
 struct Range {
   int lo, n;
@@ -240,47 +236,62 @@ __device__ inline void store_row(uint16_t *to, const float *x, int n) {
 struct Unit {
   int head, tile, lo, pages;         // kv head, tile, first page (or 0: entries of a list), pages
   int t0, fresh, kv, req, pos0;      // first token, tokens, held, request (-1: none), position of the first token
-  int64_t first;                     // index of its first page among all units' pages
+  int first;                         // index of its first page among all units' pages
 };
 
 // What the workgroups know of each request: units before it and what it takes to place its rows.
 struct Requests {
-  int64_t *prefix;            // [requests]
+  int32_t *prefix;            // [requests]
   int32_t *t0, *kv, *pos0;    // in LDS, or null: read from the step's arrays
 };
 
-// Whole units are counted instead of their pages.
+// Whole units are counted instead of their pages.  The host sees to it that all of them stay below 2^31.
 template <int TR>
-__device__ inline int64_t units_of(const KvAttnArgs &a, int fresh, int kv) {
+__device__ inline int units_of(const KvAttnArgs &a, int fresh, int kv) {
   if (fresh <= 0) return 0;
-  const int64_t n = (((int64_t)fresh * a.group + TR - 1) / TR) * a.kv_heads;
+  const int n = (int)(((int64_t)fresh * a.group + TR - 1) / TR) * a.kv_heads;
   return a.whole ? n : n * request_pages(kv, fresh, a.window, a.width).n;
+}
+
+// Position of a request's first new token.  Where the table's width has cut the request its length does not say.
+__device__ inline int first_position(const KvAttnArgs &a, int t0, int fresh, int kv) {
+  if (kv < a.width * KV_PAGE) return kv - fresh;
+  return fresh > 0 ? a.positions[t0] : 0;
+}
+
+// Sum over a wavefront's lanes up to and with the own.
+__device__ inline int lanes_up_to(int x) {
+#define KV_ADD(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false)
+  KV_ADD(0x111, 0xf);  // row_shr:1, 2, 4, 8
+  KV_ADD(0x112, 0xf);
+  KV_ADD(0x114, 0xf);
+  KV_ADD(0x118, 0xf);
+  KV_ADD(0x142, 0xa);  // row_bcast:15 into rows 1 and 3
+  KV_ADD(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
+#undef KV_ADD
+  return x;
 }
 
 // Units before every request, by the whole workgroup; returns their sum.
 template <int TR, int THREADS>
-__device__ inline int64_t scan_units(const KvAttnArgs &a, const Requests &q, int64_t *sums, int tid) {
+__device__ inline int scan_units(const KvAttnArgs &a, const Requests &q, int *sums, int tid) {
   const int lane = tid & 63, wave = tid >> 6;
-  int64_t carry = 0;
+  int carry = 0;
   for (int b = 0; b < a.requests; b += THREADS) {
     const int r = b + tid;
-    int64_t n = 0;
+    int n = 0;
     if (r < a.requests) {
       const int t0 = a.q_start[r], fresh = min(a.q_start[r + 1], a.tokens) - t0, kv = a.kv_lens[r];
       n = units_of<TR>(a, fresh, kv);
       if (q.t0) {
         q.t0[r] = t0;
         q.kv[r] = kv;
-        q.pos0[r] = fresh > 0 ? a.positions[t0] : 0;
+        q.pos0[r] = first_position(a, t0, fresh, kv);
         if (r == a.requests - 1) q.t0[r + 1] = t0 + fresh;
       }
     }
-    int64_t x = n;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up(x, d);
-      if (lane >= d) x += y;
-    }
-    __syncthreads();
+    int x = lanes_up_to(n);
+    if (b > 0) __syncthreads();
     if (lane == 63) sums[wave] = x;
     __syncthreads();
     for (int w = 0; w < wave; ++w) x += sums[w];
@@ -292,9 +303,9 @@ __device__ inline int64_t scan_units(const KvAttnArgs &a, const Requests &q, int
 }
 
 __global__ __launch_bounds__(1024) void kv_scan_kernel(KvAttnArgs a, int tile_rows) {
-  __shared__ int64_t sums[16];
+  __shared__ int sums[16];
   const Requests q = {a.prefix, nullptr, nullptr, nullptr};
-  const int64_t total = tile_rows == 16 ? scan_units<16, 1024>(a, q, sums, threadIdx.x)
+  const int total = tile_rows == 16 ? scan_units<16, 1024>(a, q, sums, threadIdx.x)
                       : tile_rows == 64 ? scan_units<64, 1024>(a, q, sums, threadIdx.x)
                       : tile_rows == 128 ? scan_units<128, 1024>(a, q, sums, threadIdx.x)
                                          : scan_units<256, 1024>(a, q, sums, threadIdx.x);
@@ -303,17 +314,16 @@ __global__ __launch_bounds__(1024) void kv_scan_kernel(KvAttnArgs a, int tile_ro
 
 // The unit that index `at` belongs to, and which of its pages that is.
 template <int TR, bool SEL>
-__device__ inline Unit unit_at(const KvAttnArgs &a, const Requests &q, int64_t at, int &offset) {
+__device__ inline Unit unit_at(const KvAttnArgs &a, const Requests &q, int at, int &offset) {
   Unit u;
-  int64_t k;  // unit of its group
+  int k;  // unit of its group
   if constexpr (SEL) {
-    const int tiles = (a.group + TR - 1) / TR, n = a.whole ? 1 : a.n_select;
-    const int64_t per = (int64_t)a.kv_heads * tiles * n;
-    u.t0 = (int)(at / per);
-    const int64_t rest = at % per;
-    k = rest / n;
-    offset = (int)(rest % n);
-    u.head = (int)(k / tiles), u.tile = (int)(k % tiles);
+    const int tiles = (a.group + TR - 1) / TR, n = a.whole ? 1 : a.n_select, per = a.kv_heads * tiles;
+    k = at / n;
+    offset = at % n;
+    u.t0 = k / per;
+    k %= per;
+    u.head = k / tiles, u.tile = k % tiles;
     u.lo = 0, u.pages = a.n_select, u.fresh = 1;
     const int r = uniform(a.token_req[u.t0]);
     u.pos0 = uniform(a.positions[u.t0]);
@@ -336,14 +346,14 @@ __device__ inline Unit unit_at(const KvAttnArgs &a, const Requests &q, int64_t a
       u.t0 = uniform(a.q_start[lo]);
       u.fresh = min(uniform(a.q_start[lo + 1]), a.tokens) - u.t0;
       u.kv = uniform(a.kv_lens[lo]);
-      u.pos0 = uniform(a.positions[u.t0]);
+      u.pos0 = uniform(first_position(a, u.t0, u.fresh, u.kv));
     }
     const Range pr = request_pages(u.kv, u.fresh, a.window, a.width);
     const int tiles = (int)(((int64_t)u.fresh * a.group + TR - 1) / TR), n = a.whole ? 1 : pr.n;
-    const int64_t rest = at - uniform(q.prefix[lo]);
+    const int rest = at - uniform(q.prefix[lo]);
     k = rest / n;
-    offset = (int)(rest % n);
-    u.head = (int)(k / tiles), u.tile = (int)(k % tiles);
+    offset = rest % n;
+    u.head = k / tiles, u.tile = k % tiles;
     u.lo = pr.lo, u.pages = pr.n;
   }
   u.first = at - offset;
@@ -352,16 +362,15 @@ __device__ inline Unit unit_at(const KvAttnArgs &a, const Requests &q, int64_t a
 
 // A workgroup's share: [begin, end) of all units' pages, or whole units.
 struct Share {
-  int64_t total, span, begin, end;
+  int span, begin, end;
 };
 
-__device__ inline Share share_of(const KvAttnArgs &a, int64_t total, int64_t wg) {
+__device__ inline Share share_of(const KvAttnArgs &a, int total, int wg) {
   Share s;
-  s.total = total;
-  s.span = a.whole ? 1 : (total + a.n_wg - 1) / a.n_wg;
-  if (!a.whole && s.span < 4) s.span = 4;
-  s.begin = wg * s.span;
-  s.end = min(s.begin + s.span, total);
+  s.span = a.whole ? 1 : max((int)(((int64_t)total + a.n_wg - 1) / a.n_wg), 4);
+  const int64_t begin = (int64_t)wg * s.span;
+  s.begin = (int)min(begin, (int64_t)total);
+  s.end = (int)min(begin + s.span, (int64_t)total);
   return s;
 }
 
@@ -370,10 +379,10 @@ __device__ inline Share share_of(const KvAttnArgs &a, int64_t total, int64_t wg)
 // share, first token, tile, kv head, rows.
 constexpr int BORDER_INTS = 8;
 
-__device__ inline void leave_border(const KvAttnArgs &a, const Share &s, const Unit &u, int64_t wg, int64_t at, int rows) {
+__device__ inline void leave_border(const KvAttnArgs &a, const Share &s, const Unit &u, int wg, int at, int rows) {
   const bool across = u.first + u.pages > s.end && u.first >= s.begin;
-  int32_t *b = a.borders + wg * BORDER_INTS;
-  b[0] = across ? (int32_t)((u.first + u.pages - 1) / s.span - wg) + 1 : 0;
+  int32_t *b = a.borders + (int64_t)wg * BORDER_INTS;
+  b[0] = across ? (u.first + u.pages - 1) / s.span - wg + 1 : 0;
   b[1] = at != s.begin;
   b[2] = u.t0;
   b[3] = u.tile;
@@ -492,30 +501,29 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   float *buf = reinterpret_cast<float *>(lds);                                     // [4][16][D + 4]
   float(*ml)[16][2] = reinterpret_cast<float(*)[16][2]>(buf + 4 * 16 * (D + 4));  // [4]
-  int64_t *sums = reinterpret_cast<int64_t *>(ml + 4);                            // [4]
+  int *sums = reinterpret_cast<int *>(ml + 4);                                    // [4]
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4;
-  const int64_t wg = blockIdx.x;
+  const int wg = blockIdx.x;
 
   Requests q = {a.prefix, nullptr, nullptr, nullptr};
-  int64_t total;
+  int total;
   if constexpr (SEL) {
-    const int tokens = a.requests > 0 ? min(a.q_start[a.requests], a.tokens) : 0;
-    total = (int64_t)tokens * a.kv_heads * ((a.group + 15) / 16) * (a.whole ? 1 : a.n_select);
+    total = a.tokens * a.kv_heads * ((a.group + 15) / 16) * (a.whole ? 1 : a.n_select);
   } else if (a.scanned) {
     total = uniform(a.prefix[a.requests]);
   } else {
     q.prefix = sums + 4;                                            // [requests], and [requests + 1] each:
-    q.t0 = reinterpret_cast<int32_t *>(q.prefix + a.requests);
+    q.t0 = q.prefix + a.requests;
     q.kv = q.t0 + a.requests + 1;
     q.pos0 = q.kv + a.requests + 1;
     total = scan_units<16, 256>(a, q, sums, tid);
   }
   const Share share = share_of(a, total, wg);
-  if (tid == 0 && !a.whole && share.begin >= share.end) a.borders[wg * BORDER_INTS] = 0;
-  for (int64_t at = share.begin; at < share.end;) {
+  if (tid == 0 && !a.whole && share.begin >= share.end) a.borders[(int64_t)wg * BORDER_INTS] = 0;
+  for (int at = share.begin; at < share.end;) {
     int offset;
     const Unit u = unit_at<16, SEL>(a, q, at, offset);
-    const int n = a.whole ? u.pages : (int)min((int64_t)u.pages - offset, share.end - at);
+    const int n = a.whole ? u.pages : min(u.pages - offset, share.end - at);
     const int rows = min(16, u.fresh * a.group - u.tile * 16);
     const Place p = place_of<16>(a, u, rows, lane & 15);
     const int32_t *table = a.table + (int64_t)max(u.req, 0) * a.width;
@@ -533,10 +541,9 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
     // the wavefront's entries offset + wave, + 4, ...: a lane looks 64 of them up at a time
     for (int k0 = offset + wave; k0 < k1; k0 += 4 * 64) {
       const int k = k0 + 4 * lane;
-      int c = -1, page = -1;
+      int c = u.lo + k, page = -1;
+      if constexpr (SEL) c = list[min(k, k1 - 1)];
       if (k < k1 && u.req >= 0) {
-        c = u.lo + k;
-        if constexpr (SEL) c = list[k];
         // not a column that no row sees anything of, nor one without a page in the cache
         if ((uint32_t)c < (uint32_t)a.width && c * KV_PAGE <= p.any_high && c * KV_PAGE + KV_PAGE - 1 > p.any_low) page = table[c];
       }
@@ -578,12 +585,12 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
     for (int ct = 0; ct < D / 16; ++ct)
       *reinterpret_cast<f32x4 *>(buf + (wave * 16 + (lane & 15)) * (D + 4) + ct * 16 + g * 4) = r.o[ct];
     __syncthreads();
-    join_waves<D, DT>(a, u, rows, n == u.pages, 2 * wg + (at != share.begin), ml, buf, tid);
-    const int64_t next = at + (a.whole ? 1 : n);
+    join_waves<D, DT>(a, u, rows, n == u.pages, 2 * (int64_t)wg + (at != share.begin), ml, buf, tid);
+    const int next = at + (a.whole ? 1 : n);
     if (tid == 0 && !a.whole && next == share.end) leave_border(a, share, u, wg, at, rows);
     at = next;
   }
-  clear_rest<D, 256>(a, wg, gridDim.x, tid);
+  if constexpr (!SEL) clear_rest<D, 256>(a, wg, gridDim.x, tid);  // (selected: rows without a request are units)
 }
 
 // Fragments of an unpacked page in LDS, 64 lanes of 16 bytes each, as the matrix units take them:
@@ -684,27 +691,27 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, W
   constexpr int TR = WAVES * NQ * 16, C = D / 32, FRAGS = page_fragments<D>(), THREADS = 64 * WAVES;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   u32x4 *frag = reinterpret_cast<u32x4 *>(lds);                              // [2][FRAGS][64]
-  int64_t *sums = reinterpret_cast<int64_t *>(frag + 2 * FRAGS * 64);        // [WAVES]
+  int *sums = reinterpret_cast<int *>(frag + 2 * FRAGS * 64);                // [WAVES]
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4;
-  const int64_t wg = blockIdx.x;
+  const int wg = blockIdx.x;
 
   Requests q = {a.prefix, nullptr, nullptr, nullptr};
-  int64_t total;
+  int total;
   if (a.scanned) {
     total = uniform(a.prefix[a.requests]);
   } else {
     q.prefix = sums + WAVES;
-    q.t0 = reinterpret_cast<int32_t *>(q.prefix + a.requests);
+    q.t0 = q.prefix + a.requests;
     q.kv = q.t0 + a.requests + 1;
     q.pos0 = q.kv + a.requests + 1;
     total = scan_units<TR, THREADS>(a, q, sums, tid);
   }
   const Share share = share_of(a, total, wg);
-  if (tid == 0 && !a.whole && share.begin >= share.end) a.borders[wg * BORDER_INTS] = 0;
-  for (int64_t at = share.begin; at < share.end;) {
+  if (tid == 0 && !a.whole && share.begin >= share.end) a.borders[(int64_t)wg * BORDER_INTS] = 0;
+  for (int at = share.begin; at < share.end;) {
     int offset;
     const Unit u = unit_at<TR, false>(a, q, at, offset);
-    const int n = a.whole ? u.pages : (int)min((int64_t)u.pages - offset, share.end - at);
+    const int n = a.whole ? u.pages : min(u.pages - offset, share.end - at);
     const int rows = min(TR, u.fresh * a.group - u.tile * TR);
     Place p[NQ];
     u32x4 qf[NQ][C];
@@ -825,7 +832,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, W
     }
 
     const bool whole = n == u.pages;
-    const int64_t slot = 2 * wg + (at != share.begin);
+    const int64_t slot = 2 * (int64_t)wg + (at != share.begin);
 #pragma unroll
     for (int k = 0; k < NQ; ++k) {
       const float l = row_sum(r[k].l);
@@ -853,7 +860,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, W
         }
       }
     }
-    const int64_t next = at + (a.whole ? 1 : n);
+    const int next = at + (a.whole ? 1 : n);
     if (tid == 0 && !a.whole && next == share.end) leave_border(a, share, u, wg, at, rows);
     at = next;
   }
@@ -954,10 +961,12 @@ Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D,
   // whole units where they are short, or (chunks) where there are many; shares otherwise: as many workgroups as the
   // chip holds at a time, four pages each at least
   const int fill = s.tile_rows == 16 ? 512 : s.tile_rows == 128 && D < 256 ? 512 : 256;
-  s.whole = narrow || (s.tile_rows > 16 && units >= 1024);
+  // (and where their pages cannot be counted in 31 bits, whatever max_new promises)
+  const int64_t surely = n_select > 0 ? n_select : window > 0 ? (window + tokens) / KV_PAGE + 2 : width;
+  s.whole = narrow || (s.tile_rows > 16 && units >= 1024) || units * (n_select > 0 || surely < width ? surely : width) > 0x7fffffff;
   s.n_wg = s.whole ? (int)units : units * most / 4 >= fill ? fill : (int)(units * most / 4 + 1);
   if (s.n_wg < 1) s.n_wg = 1;
-  s.prefix = up256((size_t)(requests + 1) * 8);
+  s.prefix = up256((size_t)(requests + 1) * 4);
   s.borders = s.whole ? 0 : up256((size_t)s.n_wg * BORDER_INTS * 4);
   s.ml = s.whole ? 0 : up256((size_t)s.n_wg * 2 * s.tile_rows * 2 * 4);
   s.o = s.whole ? 0 : up256((size_t)s.n_wg * 2 * s.tile_rows * D * 4);
@@ -979,10 +988,10 @@ int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
     hipLaunchKernelGGL(kv_scan_kernel, dim3(1), dim3(1024), 0, s, a, sh.tile_rows);
     KV_HIP_TRY(hipGetLastError());
   }
-  const size_t lists = sel || a.scanned ? 0 : (size_t)a.requests * 8 + 3 * (size_t)(a.requests + 1) * 4;
+  const size_t lists = sel || a.scanned ? 0 : ((size_t)a.requests + 3 * (size_t)(a.requests + 1)) * 4;
   int rc;
   if (sh.tile_rows == 16) {
-    const size_t lds = (size_t)(4 * 16 * (D + 4) + 4 * 16 * 2) * 4 + 4 * 8 + lists;
+    const size_t lds = (size_t)(4 * 16 * (D + 4) + 4 * 16 * 2) * 4 + 4 * 4 + lists;
     if (sel) {
       if ((rc = allow_lds(&kv_rows16_kernel<D, DT, true>, lds))) return rc;
       hipLaunchKernelGGL((kv_rows16_kernel<D, DT, true>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
@@ -991,7 +1000,7 @@ int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
       hipLaunchKernelGGL((kv_rows16_kernel<D, DT, false>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
     }
   } else {
-    const size_t lds = (size_t)2 * page_fragments<D>() * 1024 + 8 * 8 + lists;
+    const size_t lds = (size_t)2 * page_fragments<D>() * 1024 + 8 * 4 + lists;
     if constexpr (D == 256) {
       if ((rc = allow_lds(&kv_rows_kernel<D, DT, 8, 1>, lds))) return rc;
       hipLaunchKernelGGL((kv_rows_kernel<D, DT, 8, 1>), dim3((unsigned)a.n_wg), dim3(512), lds, s, a);
@@ -1039,7 +1048,7 @@ int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *works
                             a.width);
   a.n_wg = sh.n_wg;
   a.whole = sh.whole;
-  a.prefix = reinterpret_cast<int64_t *>(workspace);
+  a.prefix = reinterpret_cast<int32_t *>(workspace);
   a.borders = reinterpret_cast<int32_t *>(workspace + sh.prefix);
   a.part_ml = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders);
   a.part_o = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders + sh.ml);

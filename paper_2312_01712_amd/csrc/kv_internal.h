@@ -63,7 +63,7 @@ struct KvAttnArgs {
   int32_t negative;  // the scale was below 0
   // workgroups; whether each has a whole unit of rows instead of a share of all units' pages; whether prefix is filled
   int32_t n_wg, whole, scanned;
-  int64_t *prefix;   // [requests + 1]: units before each request, where a launch of its own scans them
+  int32_t *prefix;   // [requests + 1]: units before each request, where a launch of its own scans them
   int32_t *borders;  // [n_wg][8]: the unit that goes on in the next share
   float *part_ml;    // [2 n_wg][rows of a tile][2]: parts of units that go across borders
   float *part_o;     // [2 n_wg][rows of a tile][D]
