@@ -218,23 +218,26 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a, int tile
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.y;
   const int64_t i0 = (int64_t)blockIdx.x * tile;
-  // the tile's tokens that are the first of their run: all wavefronts look
-  bool first = false;
-  if (lane < tile && i0 + lane < a.tokens) {
-    const int64_t s = a.slots[i0 + lane];
-    first = s >= 0 && s < a.n_slots && (s % KV_PAGE == 0 || i0 + lane == 0 || a.slots[i0 + lane - 1] != s - 1);
-  }
-  uint64_t heads = __ballot(first);
+  // the slots of the tile's tokens and of the 63 behind the last, in one trip; all wavefronts look
+  const int64_t none = -2;
+  const int64_t here = i0 + lane < a.tokens ? a.slots[i0 + lane] : none;
+  const int64_t there = lane < tile && i0 + 64 + lane < a.tokens ? a.slots[i0 + 64 + lane] : none;
+  const int64_t ahead = i0 > 0 ? a.slots[i0 - 1] : none;
+  int64_t prev = __shfl_up(here, 1);
+  if (lane == 0) prev = ahead;
+  // tokens that are the first of their run
+  uint64_t heads = __ballot(lane < tile && here >= 0 && here < a.n_slots && (here % KV_PAGE == 0 || prev != here - 1));
   float low[8], high[8];
   auto keep = [&](int w) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) box[w][0][j][lane] = low[j], box[w][1][j][lane] = high[j];
   };
   for (int run = 0; heads != 0; ++run, heads &= heads - 1) {
-    const int64_t i = i0 + __builtin_ctzll(heads);
-    const int64_t slot0 = a.slots[i];
+    const int first = __builtin_ctzll(heads);
+    const int64_t i = i0 + first, slot0 = __shfl(here, first);
     // its length: a lane looks at each further place of the page
-    const bool on = lane < KV_PAGE - (int)(slot0 % KV_PAGE) && i + lane < a.tokens && a.slots[i + lane] == slot0 + lane;
+    const int64_t near = __shfl(here, (first + lane) & 63), far = __shfl(there, (first + lane) & 63);
+    const bool on = lane < KV_PAGE - (int)(slot0 % KV_PAGE) && (first + lane < 64 ? near : far) == slot0 + lane;
     const uint64_t miss = ~__ballot(on);
     const int n = miss ? __builtin_ctzll(miss) : 64;
     if (n > 16) {

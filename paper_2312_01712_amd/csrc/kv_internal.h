@@ -135,4 +135,17 @@ __device__ inline float kv_scale(uint32_t w) {
   return __uint_as_float(I == 3 ? (w >> 1) & 0x7f800000u : ((w >> (8 * I)) & 0xffu) << 23);
 }
 
+// Sum over a wavefront's lanes up to and with the own.
+__device__ inline int lanes_up_to(int x) {
+#define KV_ADD(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false)
+  KV_ADD(0x111, 0xf);  // row_shr:1, 2, 4, 8
+  KV_ADD(0x112, 0xf);
+  KV_ADD(0x114, 0xf);
+  KV_ADD(0x118, 0xf);
+  KV_ADD(0x142, 0xa);  // row_bcast:15 into rows 1 and 3
+  KV_ADD(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
+#undef KV_ADD
+  return x;
+}
+
 }  // namespace ivfpq

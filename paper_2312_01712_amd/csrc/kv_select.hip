@@ -39,17 +39,26 @@ __device__ inline void load_box(Box<D> &b, const uint16_t *at, bool there) {
   }
 }
 
-// Products of 16 rows with the boxes of 16 pages; e: the exponent of a page's unit, plus 6 + 127.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// The largest whole number that is not above x.
+__device__ inline int floor_of(float x) {
+  int v;
+  asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(v) : "v"(x));
+  return v;
+}
+
+// Products of 16 rows with the boxes of 16 pages; e: the exponent of a page's unit, plus 6 + 127.  The maxima are taken
+// with the other sign, and so are the queries that they meet: down is away from the middle for both halves of the row.
 template <int D>
 __device__ inline i32x4 box_products(const Box<D> &b, const i32x4 *qa, int lane, int &e) {
-  uint32_t top = 0;  // exponent of the page's largest corner: the four lanes of a page together
+  u16x2 most = {0, 0};  // exponent of the page's largest corner: the four lanes of a page together
 #pragma unroll
   for (int s = 0; s < 2 * D / 64; ++s)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t w = b.w[s][j >> 2][j & 3] & 0x7fff7fffu;
-      top = max(top, max(w >> 16, w & 0xffffu));
-    }
+    for (int j = 0; j < 8; ++j)
+      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, b.w[s][j >> 2][j & 3] & 0x7fff7fffu));
+  uint32_t top = max((uint32_t)most[0], (uint32_t)most[1]);
   top = max(top, (uint32_t)__shfl_xor((int)top, 16));
   top = max(top, (uint32_t)__shfl_xor((int)top, 32));
   e = (int)(top >> 7);
@@ -58,50 +67,44 @@ __device__ inline i32x4 box_products(const Box<D> &b, const i32x4 *qa, int lane,
   i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
   for (int s = 0; s < 2 * D / 64; ++s) {
-    // rounded away from the middle: down in the first half of the row, up in the second
-    const bool up = s * 64 + (lane >> 4) * 16 >= D;
-    const float f = up ? -inv : inv;
+    const float f = s * 64 + (lane >> 4) * 16 >= D ? -inv : inv;
     i32x4 x;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      uint32_t word = 0;
+      int v[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int at = w * 4 + j;
         const uint32_t two = b.w[s][at >> 3][(at & 7) >> 1];
-        const float c = __uint_as_float((at & 1) ? two & 0xffff0000u : two << 16);
-        int v = (int)floorf(c * f);
-        v = up ? -v : v;
-        word |= ((uint32_t)v & 255u) << (8 * j);
+        v[j] = floor_of(__uint_as_float((at & 1) ? two & 0xffff0000u : two << 16) * f);
       }
-      x[w] = (int)word;
+      const uint32_t low = __builtin_amdgcn_perm((uint32_t)v[1], (uint32_t)v[0], 0x0c0c0400);
+      const uint32_t high = __builtin_amdgcn_perm((uint32_t)v[3], (uint32_t)v[2], 0x04000c0c);
+      x[w] = (int)(low | high);
     }
     acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[s], x, acc, 0, 0, 0);
   }
   return acc;
 }
 
-// Rows of a tile: 16 / GP tokens that follow each other, GP query heads each (the group's, padded to a
+// Rows of a tile: `tpt` <= 16 / GP tokens that follow each other, GP query heads each (the group's, padded to a
 // power of two with its first head; above 16 heads one token, 16 heads at a time).  Tokens of different
 // requests in a tile are scored one request after the other.
 template <int D, int DT>
-__global__ __launch_bounds__(256) void kv_score_kernel(KvSelectArgs a, int GP, int chunk) {
+__global__ __launch_bounds__(256) void kv_score_kernel(KvSelectArgs a, int GP, int tpt, int chunk) {
   constexpr int KSTEPS = 2 * D / 64, C = D / 16;  // channels that a thread rounds
   __shared__ __attribute__((aligned(16))) int8_t rows[16][2 * D + 16];
   __shared__ float tops[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int h = blockIdx.y;
-  const int tpt = 16 / GP;
   const int t0 = blockIdx.x * tpt, nt = min(tpt, a.tokens - t0);
   const int row = tid >> 4, part = tid & 15;
 
   for (int g0 = 0; g0 < a.group; g0 += 16) {  // once, unless a group has more than 16 heads
-    // the rows in 8 bits, by the largest value of a token's whole group
-    float x[C], top = 0.0f;
-    for (int pass = a.group > 16 ? 0 : g0; pass <= g0 || (a.group > 16 && pass < a.group + 16); pass += 16) {
-      // groups above 16 heads: all heads for the largest value, then those of this turn
-      const bool turn = a.group <= 16 || pass >= a.group;
-      const int first = turn ? g0 : pass;
+    i32x4 qa[KSTEPS];
+    bool ready = false;
+    // a thread's channels of a row: head `first` + row % GP of the row's token, values that are not finite as 0
+    auto load_row = [&](int first, float *x) {
       const int tok = min(row / GP, nt - 1);
       int g = first + row % GP;
       if (g >= a.group) g = first;
@@ -113,35 +116,45 @@ __global__ __launch_bounds__(256) void kv_score_kernel(KvSelectArgs a, int GP, i
         const uint16_t u0 = (uint16_t)w, u1 = (uint16_t)(w >> 16);
         x[c] = KvType<DT>::not_finite(u0) ? 0.0f : KvType<DT>::to_float(u0);
         x[c + 1] = KvType<DT>::not_finite(u1) ? 0.0f : KvType<DT>::to_float(u1);
-        top = fmaxf(top, fmaxf(fabsf(x[c]), fabsf(x[c + 1])));
       }
-      if (turn) break;
-    }
-    for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    __syncthreads();
-    if (part == 0) tops[row] = top;
-    __syncthreads();
-    for (int k = row / GP * GP; k < row / GP * GP + GP; ++k) top = fmaxf(top, tops[k]);
-    float scale = 127.0f * (1.0f / top);
-    if (!(fabsf(scale) < __builtin_inff())) scale = 0.0f;
+    };
+    // the rows in 8 bits, by the largest value of a token's whole group
+    auto round_rows = [&]() {
+      float x[C], top = 0.0f;
+      if (a.group > 16)
+        for (int first = 0; first < a.group; first += 16) {
+          load_row(first, x);
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int v = (int)rintf(x[c] * scale);
-      rows[row][part * C + c] = (int8_t)(v < 0 ? v : 0);
-      rows[row][D + part * C + c] = (int8_t)(v > 0 ? v : 0);
-    }
-    __syncthreads();
-    i32x4 qa[KSTEPS];
+          for (int c = 0; c < C; ++c) top = fmaxf(top, fabsf(x[c]));
+        }
+      load_row(g0, x);
 #pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) qa[s] = *reinterpret_cast<const i32x4 *>(&rows[lane & 15][s * 64 + (lane >> 4) * 16]);
+      for (int c = 0; c < C; ++c) top = fmaxf(top, fabsf(x[c]));
+      for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+      __syncthreads();
+      if (part == 0) tops[row] = top;
+      __syncthreads();
+      for (int k = row / GP * GP; k < row / GP * GP + GP; ++k) top = fmaxf(top, tops[k]);
+      float scale = 127.0f * (1.0f / top);
+      if (!(fabsf(scale) < __builtin_inff())) scale = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int v = (int)rintf(x[c] * scale);
+        rows[row][part * C + c] = (int8_t)(v < 0 ? v : 0);
+        rows[row][D + part * C + c] = (int8_t)(v > 0 ? -v : 0);  // as the maxima: with the other sign
+      }
+      __syncthreads();
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) qa[s] = *reinterpret_cast<const i32x4 *>(&rows[lane & 15][s * 64 + (lane >> 4) * 16]);
+    };
 
     for (int k0 = 0, k1; k0 < nt; k0 = k1) {  // tokens k0 .. k1 of one request
       const int r = a.token_req[t0 + k0];
-      for (k1 = k0 + 1; k1 < nt && a.token_req[t0 + k1] == r; ++k1) {}
-      if ((uint32_t)r >= (uint32_t)a.requests) continue;
-      const int pos_last = a.positions[t0 + k1 - 1];
-      const int visible = pos_last < 0 ? 0 : min(pos_last / KV_PAGE + 1, a.width);
+      int pos_last = a.positions[t0 + k0];
+      for (k1 = k0 + 1; k1 < nt && a.token_req[t0 + k1] == r; ++k1) pos_last = a.positions[t0 + k1];
+      const int visible = (uint32_t)r >= (uint32_t)a.requests || pos_last < 0 ? 0 : min(pos_last / KV_PAGE + 1, a.width);
       const int p0 = blockIdx.z * chunk, p1 = min(p0 + chunk, visible);
+      if (p0 >= p1) continue;
       const int32_t *table = a.table + (int64_t)r * a.width;
       // two tiles of pages ahead: their numbers, and one box
       auto number = [&](int pb) -> int32_t {
@@ -179,6 +192,8 @@ __global__ __launch_bounds__(256) void kv_score_kernel(KvSelectArgs a, int GP, i
       int pb = p0 + wave * 16;
       int32_t page = number(pb), next = number(pb + SCORE_PAGES);
       if (pb < p1) fetch(even, page);
+      if (!ready) round_rows();  // while the first boxes are on their way
+      ready = true;
       for (; pb < p1; pb += 2 * SCORE_PAGES) {
         const int32_t third = number(pb + 2 * SCORE_PAGES), fourth = number(pb + 3 * SCORE_PAGES);
         fetch(odd, next);
@@ -200,34 +215,36 @@ __device__ inline uint32_t key_of(float s) {
 }
 
 constexpr int PICK_BINS = 2048;
+constexpr int PICK_LAST = 64;  // keys of the last bin that are ranked one by one
 
-// Inclusive sums over the workgroup, in thread order.
+// Sum over the workgroup in thread order, up to and with the own; all: of everything.
 template <int THREADS>
-__device__ inline int block_sum(int x, int *sums, int tid) {
+__device__ inline int block_sum(int x, int *sums, int tid, int &all) {
   const int lane = tid & 63, wave = tid >> 6;
-  for (int d = 1; d < 64; d <<= 1) {
-    const int u = __shfl_up(x, d);
-    if (lane >= d) x += u;
-  }
+  x = lanes_up_to(x);
   __syncthreads();  // the sums of a call before are read
   if (lane == 63) sums[wave] = x;
   __syncthreads();
-  for (int w = 0; w < wave; ++w) x += sums[w];
-  return x;
+  const int before = lanes_up_to(lane < THREADS / 64 ? sums[lane] : 0);
+  all = __builtin_amdgcn_readlane(before, THREADS / 64 - 1);
+  const int w = __builtin_amdgcn_readfirstlane(wave);
+  return w > 0 ? x + __builtin_amdgcn_readlane(before, w - 1) : x;
 }
 
 // The columns of one token and head, four a thread and turn.  The n-th largest key: counts of the keys in
 // 2048 bins between the smallest and the largest (the scores of a context lie within a few octaves,
-// so that bins of equal width spread them), then again within the bin that holds it, 11 bits a time.
-// Up to TURNS * 4 * THREADS columns keep their keys in registers, more are read again.
-// Bound by the latency of its few dependent steps (4094 columns: 20.7 us with four counts of 8 bits, whose
-// first digit is the same for all).
+// so that bins of equal width spread them); the few keys of the bin that holds it are ranked one by one, many
+// are counted again, 11 bits a time.  Up to TURNS * 4 * THREADS columns keep their keys in registers, more
+// are read again.  Bound by the latency of its dependent steps (4094 columns: 20.7 us with four counts
+// of 8 bits, whose first digit is the same for all).
 template <int THREADS, int TURNS>
 __global__ __launch_bounds__(THREADS) void kv_pick_kernel(KvSelectArgs a) {
   __shared__ int counts[PICK_BINS];
   __shared__ int sums[THREADS / 64];
   __shared__ uint32_t range[2][THREADS / 64];
-  __shared__ int found[2];
+  __shared__ int found[3];
+  __shared__ uint32_t last_key[PICK_LAST];
+  __shared__ int last_col[PICK_LAST], last_n;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.x;
   const int h = blockIdx.y, n = a.n_select;
@@ -260,6 +277,8 @@ __global__ __launch_bounds__(THREADS) void kv_pick_kernel(KvSelectArgs a) {
       f(b + tid * 4, k);
     }
   };
+  for (int b = tid; b < PICK_BINS; b += THREADS) counts[b] = 0;
+  if (tid == 0) last_n = 0;
   uint32_t lo = 0xffffffffu, hi = 0;
   each([&](int i, const uint32_t (&k)[4]) {
     for (int j = 0; j < 4; ++j)
@@ -272,73 +291,99 @@ __global__ __launch_bounds__(THREADS) void kv_pick_kernel(KvSelectArgs a) {
   if (lane == 0) range[0][wave] = lo, range[1][wave] = hi;
   __syncthreads();
   for (int w = 0; w < THREADS / 64; ++w) lo = min(lo, range[0][w]), hi = max(hi, range[1][w]);
-  // keys above `limit` are in, and of those equal to it the first `left`
-  int left = n - a.sinks - a.recent;
+  // ranked keys above `limit` are in, and those equal to it up to column `limit_col`
+  int left = n - a.sinks - a.recent, limit_col = -1, all;
   uint32_t limit = 0xffffffffu;
-  if (left > 0) {
-    for (;;) {
-      const uint32_t width = hi - lo;
-      const int shift = width < PICK_BINS ? 0 : 32 - __clz((int)width) - 11;
-      for (int b = tid; b < PICK_BINS; b += THREADS) counts[b] = 0;
-      __syncthreads();
+  while (left > 0) {
+    const uint32_t width = hi - lo;
+    const int shift = width < PICK_BINS ? 0 : 32 - __clz((int)width) - 11;
+    each([&](int i, const uint32_t (&k)[4]) {
+      for (int j = 0; j < 4; ++j)
+        if (ranked(i + j) && k[j] >= lo && k[j] <= hi) atomicAdd(&counts[(k[j] - lo) >> shift], 1);
+    });
+    __syncthreads();
+    // from the highest bin down: the one at which the count reaches `left`
+    constexpr int PER = PICK_BINS / THREADS;
+    int c[PER], sum = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) c[j] = counts[PICK_BINS - 1 - (tid * PER + j)], sum += c[j];
+    int before = block_sum<THREADS>(sum, sums, tid, all) - sum;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      if (before < left && before + c[j] >= left)
+        found[0] = PICK_BINS - 1 - (tid * PER + j), found[1] = left - before, found[2] = c[j];
+      before += c[j];
+      counts[PICK_BINS - 1 - (tid * PER + j)] = 0;  // for another turn
+    }
+    __syncthreads();
+    lo += (uint32_t)found[0] << shift;
+    hi = min(hi, lo + ((1u << shift) - 1));
+    left = found[1];
+    const int in_bin = found[2];
+    if (in_bin <= PICK_LAST) {
+      // all of the bin: in it, the `left`-th by (key down, column up)
       each([&](int i, const uint32_t (&k)[4]) {
         for (int j = 0; j < 4; ++j)
-          if (ranked(i + j) && k[j] >= lo && k[j] <= hi) atomicAdd(&counts[(k[j] - lo) >> shift], 1);
+          if (ranked(i + j) && k[j] >= lo && k[j] <= hi) {
+            const int at = atomicAdd(&last_n, 1);
+            last_key[at] = k[j];
+            last_col[at] = i + j;
+          }
       });
       __syncthreads();
-      // from the highest bin down: the one at which the count reaches `left`
-      constexpr int PER = PICK_BINS / THREADS;
-      int c[PER], sum = 0;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) c[j] = counts[PICK_BINS - 1 - (tid * PER + j)], sum += c[j];
-      int before = block_sum<THREADS>(sum, sums, tid) - sum;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        if (before < left && before + c[j] >= left) found[0] = PICK_BINS - 1 - (tid * PER + j), found[1] = left - before;
-        before += c[j];
+      if (wave == 0) {
+        const uint32_t key = lane < in_bin ? last_key[lane] : 0;
+        const int col = lane < in_bin ? last_col[lane] : 0x7fffffff;
+        int rank = 0;
+        for (int j = 0; j < in_bin; ++j) {
+          const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key, j);
+          const int c2 = __builtin_amdgcn_readlane(col, j);
+          rank += k > key || (k == key && c2 < col);
+        }
+        if (lane < in_bin && rank == left - 1) found[0] = (int)key, found[1] = col;
       }
       __syncthreads();
-      const uint32_t bin = (uint32_t)found[0];
-      left = found[1];
-      lo += bin << shift;
-      hi = min(hi, lo + ((1u << shift) - 1));
-      __syncthreads();
-      if (lo == hi) break;
+      limit = (uint32_t)found[0];
+      limit_col = found[1];
+      break;
     }
-    limit = lo;
+    if (lo == hi) {
+      // many equal keys: the first `left` of them, found by counting in order
+      int seen = 0;
+      each([&](int i, const uint32_t (&k)[4]) {
+        int eq = 0;
+        for (int j = 0; j < 4; ++j) eq += ranked(i + j) && k[j] == lo;
+        int e = seen + block_sum<THREADS>(eq, sums, tid, all) - eq;
+        for (int j = 0; j < 4; ++j)
+          if (ranked(i + j) && k[j] == lo && ++e == left) found[1] = i + j;
+        seen += all;
+      });
+      __syncthreads();
+      limit = lo;
+      limit_col = found[1];
+      break;
+    }
+    __syncthreads();  // found is read before it is written again
   }
-  // in order: the first and last columns, all keys above the limit, and the first `left` of those equal to it
-  int equals = 0, chosen = 0;  // before this turn
+  int chosen = 0;  // before this turn
   each([&](int i, const uint32_t (&k)[4]) {
-    int eq = 0, in = 0;
+    bool in[4];
+    int count = 0;
+    for (int j = 0; j < 4; ++j) {
+      in[j] = i + j < visible && (!ranked(i + j) || (left > 0 && (k[j] > limit || (k[j] == limit && i + j <= limit_col))));
+      count += in[j];
+    }
+    int at = chosen + block_sum<THREADS>(count, sums, tid, all) - count;
     for (int j = 0; j < 4; ++j)
-      if (i + j < visible) {
-        const bool forced = !ranked(i + j);
-        eq += !forced && left > 0 && k[j] == limit;
-        in += forced || (left > 0 && k[j] > limit);
-      }
-    // two counts in one sum: both are below 2^15 in a turn
-    const int both = block_sum<THREADS>(in | eq << 16, sums, tid);
-    int e = equals + (both >> 16) - eq, at = chosen + (both & 0xffff) - in;
-    for (int j = 0; j < 4; ++j)
-      if (i + j < visible) {
-        const bool forced = !ranked(i + j);
-        const bool same = !forced && left > 0 && k[j] == limit;
-        if (forced || (left > 0 && k[j] > limit) || (same && e < left)) out[at + min(e, left)] = i + j;
-        if (same) ++e;
-        else at += forced || (left > 0 && k[j] > limit);
-      }
-    int last = 0;
-    for (int w = 0; w < THREADS / 64; ++w) last += sums[w];
-    equals += last >> 16;
-    chosen += last & 0xffff;
+      if (in[j]) out[at++] = i + j;
+    chosen += all;
   });
 }
 
 template <int D>
-void score_of(const KvSelectArgs &a, int dtype, dim3 grid, int GP, int chunk, hipStream_t s) {
-  if (dtype == IVFPQ_KV_BF16) hipLaunchKernelGGL((kv_score_kernel<D, IVFPQ_KV_BF16>), grid, dim3(256), 0, s, a, GP, chunk);
-  else hipLaunchKernelGGL((kv_score_kernel<D, IVFPQ_KV_FP16>), grid, dim3(256), 0, s, a, GP, chunk);
+void score_of(const KvSelectArgs &a, int dtype, dim3 grid, int GP, int tpt, int chunk, hipStream_t s) {
+  if (dtype == IVFPQ_KV_BF16) hipLaunchKernelGGL((kv_score_kernel<D, IVFPQ_KV_BF16>), grid, dim3(256), 0, s, a, GP, tpt, chunk);
+  else hipLaunchKernelGGL((kv_score_kernel<D, IVFPQ_KV_FP16>), grid, dim3(256), 0, s, a, GP, tpt, chunk);
 }
 
 }  // namespace
@@ -347,16 +392,18 @@ int launch_kv_select(const KvSelectArgs &a, int D, int dtype, hipStream_t s) {
   if (a.requests > 0 && a.width > a.n_select) {
     int GP = 1;
     while (GP < a.group && GP < 16) GP <<= 1;
-    const int64_t tiles = (a.tokens + 16 / GP - 1) / (16 / GP);
+    // one token a tile where a request has one (a tile would have its requests' pages one after the other)
+    const int tpt = a.tokens <= a.requests ? 1 : 16 / GP;
+    const int64_t tiles = (a.tokens + tpt - 1) / tpt;
     // pages of a workgroup: two turns of its wavefronts, more where that would be a great many workgroups
     int64_t chunk = 2 * SCORE_PAGES;
     while (chunk < 1024 && tiles * a.kv_heads * ((a.width + chunk - 1) / chunk) > 16384) chunk *= 2;
     const dim3 grid((unsigned)tiles, (unsigned)a.kv_heads, (unsigned)((a.width + chunk - 1) / chunk));
     switch (D) {
-      case 64: score_of<64>(a, dtype, grid, GP, (int)chunk, s); break;
-      case 96: score_of<96>(a, dtype, grid, GP, (int)chunk, s); break;
-      case 128: score_of<128>(a, dtype, grid, GP, (int)chunk, s); break;
-      default: score_of<256>(a, dtype, grid, GP, (int)chunk, s); break;
+      case 64: score_of<64>(a, dtype, grid, GP, tpt, (int)chunk, s); break;
+      case 96: score_of<96>(a, dtype, grid, GP, tpt, (int)chunk, s); break;
+      case 128: score_of<128>(a, dtype, grid, GP, tpt, (int)chunk, s); break;
+      default: score_of<256>(a, dtype, grid, GP, tpt, (int)chunk, s); break;
     }
     KV_HIP_TRY(hipGetLastError());
   }
