@@ -199,6 +199,10 @@ int ivfpq_kv_select(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, ivfpq_kv_ro
     return IVFPQ_ERR_INVALID_ARGUMENT;
   }
   if (s->max_tokens == 0) return IVFPQ_OK;
+  if ((int64_t)s->max_tokens * c->kv_heads * (s->table_width / 1024 + 1) > 0x7fffffff) {
+    set_error("%s: max_tokens * kv_heads * table_width is too large for one launch", fn);
+    return IVFPQ_ERR_UNSUPPORTED;
+  }
   rc = check_step_arrays(s, fn);
   if (rc) return rc;
   rc = check_rows(q.data, q.token_stride, q.head_stride, s->max_tokens, heads, "q", fn);

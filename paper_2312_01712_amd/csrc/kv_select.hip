@@ -96,8 +96,10 @@ __global__ __launch_bounds__(256) void kv_score_kernel(KvSelectArgs a, int GP, i
   __shared__ __attribute__((aligned(16))) int8_t rows[16][2 * D + 16];
   __shared__ float tops[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int h = blockIdx.y;
-  const int t0 = blockIdx.x * tpt, nt = min(tpt, a.tokens - t0);
+  // the heads of a page's boxes lie next to each other: their workgroups run beside each other
+  const int tiles = (a.tokens + tpt - 1) / tpt, h = blockIdx.x % a.kv_heads;
+  const int tile = blockIdx.x / a.kv_heads % tiles, part_of = blockIdx.x / a.kv_heads / tiles;
+  const int t0 = tile * tpt, nt = min(tpt, a.tokens - t0);
   const int row = tid >> 4, part = tid & 15;
 
   for (int g0 = 0; g0 < a.group; g0 += 16) {  // once, unless a group has more than 16 heads
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(256) void kv_score_kernel(KvSelectArgs a, int GP, i
       int pos_last = a.positions[t0 + k0];
       for (k1 = k0 + 1; k1 < nt && a.token_req[t0 + k1] == r; ++k1) pos_last = a.positions[t0 + k1];
       const int visible = (uint32_t)r >= (uint32_t)a.requests || pos_last < 0 ? 0 : min(pos_last / KV_PAGE + 1, a.width);
-      const int p0 = blockIdx.z * chunk, p1 = min(p0 + chunk, visible);
+      const int p0 = part_of * chunk, p1 = min(p0 + chunk, visible);
       if (p0 >= p1) continue;
       const int32_t *table = a.table + (int64_t)r * a.width;
       // two tiles of pages ahead: their numbers, and one box
@@ -398,7 +400,7 @@ int launch_kv_select(const KvSelectArgs &a, int D, int dtype, hipStream_t s) {
     // pages of a workgroup: two turns of its wavefronts, more where that would be a great many workgroups
     int64_t chunk = 2 * SCORE_PAGES;
     while (chunk < 1024 && tiles * a.kv_heads * ((a.width + chunk - 1) / chunk) > 16384) chunk *= 2;
-    const dim3 grid((unsigned)tiles, (unsigned)a.kv_heads, (unsigned)((a.width + chunk - 1) / chunk));
+    const dim3 grid((unsigned)(tiles * a.kv_heads * ((a.width + chunk - 1) / chunk)));
     switch (D) {
       case 64: score_of<64>(a, dtype, grid, GP, tpt, (int)chunk, s); break;
       case 96: score_of<96>(a, dtype, grid, GP, tpt, (int)chunk, s); break;
