@@ -12,10 +12,10 @@ namespace ivfpq {
 
 namespace {
 
-// max over the four lanes that share 32 channels (they are aligned to four)
-__device__ inline float quad_max(float x) {
-  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true)));
-  return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x4E, 0xf, 0xf, true)));
+// over the four lanes that share 32 channels (they are aligned to four)
+__device__ inline uint32_t quad_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, true));
+  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true));
 }
 
 // the value of the lane two further within its four
@@ -23,26 +23,32 @@ __device__ inline uint32_t quad_across(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true);
 }
 
-// eight values as codes, the first channel lowest; b: the scale byte of the 32 channels
-template <int DT>
-__device__ inline uint32_t round_row(u32x4 raw, bool bad, uint32_t &b) {
-  float x[8], top = 0.0f;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Bits of the largest size among eight values: sizes order like their bits, infinities and NaN come last.
+__device__ inline uint32_t largest(u32x4 raw) {
+  u16x2 m = __builtin_bit_cast(u16x2, raw[0] & 0x7fff7fffu);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    x[j] = KvType<DT>::to_float((uint16_t)(raw[j >> 1] >> (16 * (j & 1))));
-    if (bad) x[j] = 0.0f;
-    top = fmaxf(top, fabsf(x[j]));
-  }
-  top = quad_max(top);
-  int e = (int)(__float_as_uint(top) >> 23) - 2;
-  e = e < 1 ? 1 : e > 254 ? 254 : e;
-  b = (uint32_t)e;
+  for (int j = 1; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, raw[j] & 0x7fff7fffu));
+  return max((uint32_t)m[0], (uint32_t)m[1]);
+}
+
+// The scale byte of 32 channels whose largest size has these bits.
+template <int DT>
+__device__ inline uint32_t scale_of(uint32_t top) {
+  const int e = (int)(__float_as_uint(KvType<DT>::to_float((uint16_t)top)) >> 23) - 2;
+  return (uint32_t)(e < 1 ? 1 : e > 254 ? 254 : e);
+}
+
+// eight values as codes, the first channel lowest
+template <int DT>
+__device__ inline uint32_t round_row(u32x4 raw, uint32_t b) {
   const float scale = __uint_as_float(b << 23);
   uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+  w = KvType<DT>::template round<0>(w, raw[0], scale);
+  w = KvType<DT>::template round<1>(w, raw[1], scale);
+  w = KvType<DT>::template round<2>(w, raw[2], scale);
+  w = KvType<DT>::template round<3>(w, raw[3], scale);
   return w;
 }
 
@@ -57,13 +63,10 @@ __device__ inline u32x4 held_row(uint32_t w, uint32_t b) {
   return r;
 }
 
-template <int DT>
-__device__ inline bool row_bad(u32x4 raw) {
-  bool bad = false;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    bad = bad || KvType<DT>::not_finite((uint16_t)raw[j]) || KvType<DT>::not_finite((uint16_t)(raw[j] >> 16));
-  return bad;
+// four nibbles to the low halves of four bytes
+__device__ inline uint32_t spread(uint32_t x) {
+  x = (x | (x << 8)) & 0x00ff00ffu;
+  return (x | (x << 4)) & 0x0f0f0f0fu;
 }
 
 // A run's tokens whose places p have (p / STEP) % of == turn: codes, scales, rounded rows; the lane's eight channels' box.
@@ -88,6 +91,8 @@ __device__ inline void write_run(const KvAppendArgs &a, int64_t i, int64_t slot0
   // groups of four places, from the one that holds the first token
   for (int g0 = (place0 & ~3) + turn * STEP; g0 < place0 + n; g0 += of * STEP) {
     const int t0 = g0 + quad * 4;  // place of the lane's first token
+    const int64_t row0 = i + t0 - place0;
+    const uint16_t *kr0 = kp + row0 * a.k_token, *vr0 = vp + row0 * a.v_token;
     u32x4 kr[4], vr[4];
     bool in[4];
 #pragma unroll
@@ -97,20 +102,32 @@ __device__ inline void write_run(const KvAppendArgs &a, int64_t i, int64_t slot0
       kr[j] = u32x4{0, 0, 0, 0};
       vr[j] = u32x4{0, 0, 0, 0};
       if (in[j]) {
-        const int64_t row = i + place - place0;
-        kr[j] = *reinterpret_cast<const u32x4 *>(kp + row * a.k_token);
-        vr[j] = *reinterpret_cast<const u32x4 *>(vp + row * a.v_token);
+        kr[j] = *reinterpret_cast<const u32x4 *>(kr0 + j * a.k_token);
+        vr[j] = *reinterpret_cast<const u32x4 *>(vr0 + j * a.v_token);
       }
     }
     uint32_t kc[4], vc[4], ks[4], vs[4];
-    bool any = false;
+    bool bad[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool bad = (__ballot(row_bad<DT>(kr[j]) || row_bad<DT>(vr[j])) & token_mask) != 0;
-      kc[j] = round_row<DT>(kr[j], bad, ks[j]);
-      vc[j] = round_row<DT>(vr[j], bad, vs[j]);
+      uint32_t kt = largest(kr[j]), vt = largest(vr[j]);
+      const uint64_t hit = __ballot(max(kt, vt) >= KvType<DT>::not_finite_bits);
+      bad[j] = (hit & token_mask) != 0;
+      if (hit != 0) {  // a token of this wavefront; zeros in the place of its values
+        if (bad[j]) {
+          kr[j] = vr[j] = u32x4{0, 0, 0, 0};
+          kt = vt = 0;
+        }
+      }
+      ks[j] = scale_of<DT>(quad_max(kt));
+      vs[j] = scale_of<DT>(quad_max(vt));
+      kc[j] = round_row<DT>(kr[j], ks[j]);
+      vc[j] = round_row<DT>(vr[j], vs[j]);
+    }
+    const int64_t out0 = (row0 * a.kv_heads + h) * D + oct * 8, out_step = (int64_t)a.kv_heads * D;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
       if (in[j]) {
-        any = true;
         const int place = t0 + j;
         const u32x4 kh = held_row<DT>(kc[j], ks[j]);
 #pragma unroll
@@ -121,58 +138,47 @@ __device__ inline void write_run(const KvAppendArgs &a, int64_t i, int64_t slot0
         }
         *reinterpret_cast<uint32_t *>(at + place * (D / 2) + oct * 4) = kc[j];
         if ((oct & 3) == 0)
-          at[kv_kscale_at(D) + ((place % 16) * (D / 32) + group) * 4 + place / 16] = (char)(bad ? 255 : ks[j]);
+          at[kv_kscale_at(D) + ((place % 16) * (D / 32) + group) * 4 + place / 16] = (char)(bad[j] ? 255 : ks[j]);
         if (a.k_rounded) {
-          const int64_t row = ((i + place - place0) * a.kv_heads + h) * D + oct * 8;
           const u32x4 nan = u32x4{0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
-          *reinterpret_cast<u32x4 *>(a.k_rounded + row) = bad ? nan : kh;
+          *reinterpret_cast<u32x4 *>(a.k_rounded + out0 + j * out_step) = bad[j] ? nan : kh;
         }
-        if (a.v_rounded) {
-          const int64_t row = ((i + place - place0) * a.kv_heads + h) * D + oct * 8;
-          *reinterpret_cast<u32x4 *>(a.v_rounded + row) = held_row<DT>(vc[j], vs[j]);
-        }
+        if (a.v_rounded) *reinterpret_cast<u32x4 *>(a.v_rounded + out0 + j * out_step) = held_row<DT>(vc[j], vs[j]);
       }
-    }
     // values: a byte has channels c and c + 16 of one token; the lane two further has the other
-    // nibbles, and each of the two writes four of the eight bytes
+    // nibbles, and each of the two writes four of the eight bytes: channels 0-3 of the octet the
+    // lower lane, 4-7 the upper one
     const bool upper = (oct & 2) != 0;  // this lane's channels are the high nibbles
-    uint32_t bytes[4];                  // byte c: this lane's c-th of the four, per token
+    uint32_t bytes[4];                  // a token's four bytes
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t other = quad_across(vc[j]);
-      const uint32_t lo = upper ? other : vc[j], hi = upper ? vc[j] : other;
-      // channels 0-3 of the octet for the lower lane, 4-7 for the upper one
-      const uint32_t l = (upper ? lo >> 16 : lo) & 0xffff, u = (upper ? hi >> 16 : hi) & 0xffff;
-      uint32_t w = 0;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) w |= (((l >> (4 * c)) & 15) | (((u >> (4 * c)) & 15) << 4)) << (8 * c);
-      bytes[j] = w;
+      const uint32_t lo = upper ? other >> 16 : vc[j] & 0xffff, hi = upper ? vc[j] >> 16 : other & 0xffff;
+      bytes[j] = spread(lo) | (spread(hi) << 4);
     }
-    if (any) {
-      const bool whole = in[0] && in[1] && in[2] && in[3];
-      char *base = at + kv_v_at(D) + group * 1024 + ((t0 / 4) % 4) * 256 + (t0 / 16) * 4;
-      const int c16 = (oct & 1) * 8 + (upper ? 4 : 0);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        char *to = base + (c16 + c) * 16;
-        if (whole) {
-          *reinterpret_cast<uint32_t *>(to) = ((bytes[0] >> (8 * c)) & 255) | (((bytes[1] >> (8 * c)) & 255) << 8) |
-                                              (((bytes[2] >> (8 * c)) & 255) << 16) | (((bytes[3] >> (8 * c)) & 255) << 24);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (in[j]) to[j] = (char)(bytes[j] >> (8 * c));
-        }
-      }
-      if ((oct & 3) == 0) {
-        char *to = at + kv_vscale_at(D) + group * 64 + ((t0 / 4) % 4) * 16 + (t0 / 16) * 4;
+    if (in[0] || in[1] || in[2] || in[3]) {
+      char *base = at + kv_v_at(D) + group * 1024 + ((t0 / 4) % 4) * 256 + (t0 / 16) * 4 + ((oct & 1) * 8 + (upper ? 4 : 0)) * 16;
+      char *scales = at + kv_vscale_at(D) + group * 64 + ((t0 / 4) % 4) * 16 + (t0 / 16) * 4;
+      if (in[0] && in[1] && in[2] && in[3]) {
+        // four tokens' bytes of a channel together
+        const uint32_t a01 = __builtin_amdgcn_perm(bytes[1], bytes[0], 0x05010400), b01 = __builtin_amdgcn_perm(bytes[1], bytes[0], 0x07030602);
+        const uint32_t a23 = __builtin_amdgcn_perm(bytes[3], bytes[2], 0x05010400), b23 = __builtin_amdgcn_perm(bytes[3], bytes[2], 0x07030602);
+        *reinterpret_cast<uint32_t *>(base) = __builtin_amdgcn_perm(a23, a01, 0x05040100);
+        *reinterpret_cast<uint32_t *>(base + 16) = __builtin_amdgcn_perm(a23, a01, 0x07060302);
+        *reinterpret_cast<uint32_t *>(base + 32) = __builtin_amdgcn_perm(b23, b01, 0x05040100);
+        *reinterpret_cast<uint32_t *>(base + 48) = __builtin_amdgcn_perm(b23, b01, 0x07060302);
+        if ((oct & 3) == 0) *reinterpret_cast<uint32_t *>(scales) = vs[0] | (vs[1] << 8) | (vs[2] << 16) | (vs[3] << 24);
+      } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (in[j]) to[j] = (char)vs[j];
+          if (in[j]) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) base[c * 16 + j] = (char)(bytes[j] >> (8 * c));
+            if ((oct & 3) == 0) scales[j] = (char)vs[j];
+          }
       }
     }
   }
-
 }
 
 // The lanes' boxes of a run, and of `waves` wavefronts, joined with what the page's earlier tokens left.

@@ -92,6 +92,7 @@ struct KvType<IVFPQ_KV_BF16> {
   typedef __bf16 x2 __attribute__((ext_vector_type(2)));
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
   static __device__ inline float to_float(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
+  static constexpr uint32_t not_finite_bits = 0x7f80;  // sizes from here on are infinite or NaN
   static __device__ inline bool not_finite(uint16_t u) { return (u & 0x7f80) == 0x7f80; }
   static __device__ inline uint32_t pack(float a, float b) {
     typedef float f2 __attribute__((ext_vector_type(2)));
@@ -102,6 +103,11 @@ struct KvType<IVFPQ_KV_BF16> {
   template <int SEL>
   static __device__ inline uint32_t unpack(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
+  }
+  // two values, divided by the scale and rounded, into byte SEL of w
+  template <int SEL>
+  static __device__ inline uint32_t round(uint32_t w, uint32_t two, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(x2, two), scale, SEL);
   }
   static __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -114,6 +120,7 @@ struct KvType<IVFPQ_KV_FP16> {
   typedef _Float16 x2 __attribute__((ext_vector_type(2)));
   typedef _Float16 x8 __attribute__((ext_vector_type(8)));
   static __device__ inline float to_float(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
+  static constexpr uint32_t not_finite_bits = 0x7c00;
   static __device__ inline bool not_finite(uint16_t u) { return (u & 0x7c00) == 0x7c00; }
   static __device__ inline uint32_t pack(float a, float b) {
     typedef float f2 __attribute__((ext_vector_type(2)));
@@ -123,6 +130,10 @@ struct KvType<IVFPQ_KV_FP16> {
   template <int SEL>
   static __device__ inline uint32_t unpack(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, SEL));
+  }
+  template <int SEL>
+  static __device__ inline uint32_t round(uint32_t w, uint32_t two, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(x2, two), scale, SEL);
   }
   static __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
