@@ -37,6 +37,7 @@ __device__ inline int64_t wave_sum(int64_t v) {
 }
 
 constexpr int PLAN_PER_GROUP = 64;  // most requests that a workgroup owns
+constexpr int WIDE = 256;           // pages given back by more than one wavefront
 
 __global__ __launch_bounds__(256) void kv_plan_kernel(KvPlanArgs a) {
   __shared__ int64_t before[3], sums[4][3];
@@ -45,13 +46,24 @@ __global__ __launch_bounds__(256) void kv_plan_kernel(KvPlanArgs a) {
   const int r0 = blockIdx.x * a.per_group, part = blockIdx.y;
   const int n_own = min(a.per_group, a.requests - r0);
 
+  // eight requests a thread in flight: their lengths are in L2 and what counts is the trip to it
   int64_t s0 = 0, s1 = 0, s2 = 0;
-#pragma unroll 4
-  for (int r = tid; r < r0; r += 256) {
-    const Counts c = counts_of(a.past[r], a.fresh[r], a.width);
-    s0 += c.fresh;
-    s1 += c.take;
-    s2 += c.give;
+  for (int b = 0; b < r0; b += 8 * 256) {
+    int32_t past[8], fresh[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int r = min(b + k * 256 + tid, r0);  // (request r0 exists)
+      past[k] = a.past[r];
+      fresh[k] = a.fresh[r];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (b + k * 256 + tid < r0) {
+        const Counts c = counts_of(past[k], fresh[k], a.width);
+        s0 += c.fresh;
+        s1 += c.take;
+        s2 += c.give;
+      }
   }
   s0 = wave_sum(s0);
   s1 = wave_sum(s1);
@@ -103,6 +115,31 @@ __global__ __launch_bounds__(256) void kv_plan_kernel(KvPlanArgs a) {
     a.q_start[a.requests] = (int32_t)min(before[0], (int64_t)a.max_tokens);
   }
 
+  // pages of an ended request, from `first` on every `stride`-th: eight loads on their way at a time
+  auto give_back = [&](const int32_t *row, int32_t before_it, int32_t n, int first, int stride) {
+    for (int b = first; b < n; b += 8 * stride) {
+      int32_t page[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) page[k] = row[min(b + k * stride, n - 1)];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int j = b + k * stride;
+        const int64_t to = (int64_t)before_it + j;
+        if (j < n && to < a.capacity) {
+          int64_t at = tail_at + to;
+          if (at >= cap) at -= cap;
+          a.free_pages[at] = page[k];
+        }
+      }
+    }
+  };
+  // many pages: the whole workgroup on a request
+  if (a.parts == 1)
+    for (int i = 0; i < n_own; ++i) {
+      const Counts c = counts_of(own[i][3], own[i][4], a.width);
+      if (c.give > WIDE) give_back(a.table + (int64_t)(r0 + i) * a.width, own[i][2], c.give, tid, 256);
+    }
+
   const int n_waves = 4 * a.parts, w = part * 4 + wave;  // all of them on one request after the other when there are few
   for (int i = a.parts == 1 ? wave : 0; i < n_own; i += a.parts == 1 ? 4 : 1) {
     const int r = r0 + i, first = a.parts == 1 ? lane : w * 64 + lane, stride = a.parts == 1 ? 64 : n_waves * 64;
@@ -117,14 +154,7 @@ __global__ __launch_bounds__(256) void kv_plan_kernel(KvPlanArgs a) {
       if (at >= cap) at -= cap;
       return a.free_pages[at];
     };
-    for (int j = first; j < c.give; j += stride) {
-      const int64_t n = (int64_t)own[i][2] + j;
-      if (n < a.capacity) {
-        int64_t at = tail_at + n;
-        if (at >= cap) at -= cap;
-        a.free_pages[at] = row[j];
-      }
-    }
+    if (c.give <= WIDE || a.parts > 1) give_back(row, own[i][2], c.give, first, stride);
     for (int j = first; j < c.take; j += stride) row[c.held + j] = taken(j);
     for (int64_t j = first; j < c.fresh; j += stride) {
       const int64_t t = own[i][0] + j, pos = c.past + j;
