@@ -588,3 +588,15 @@ def test_refusals(kv):
             call()
         assert e.value.status == status, e.value
     torch.cuda.synchronize()
+
+
+def test_the_example_runs(kv):
+    """examples/kv_decode.py, small: all operators together; looking at every page is attention over everything."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import kv_decode
+    whole, part = kv_decode.main(["--requests", "3", "--prompt", "300", "--steps", "3", "--pages", "8"])
+    assert torch.isfinite(whole).all()
+    # the same keys in another order of sums: within a few units of the weights' and results' rounding
+    assert (whole - part).float().abs().max() <= 2.0 ** -5 * whole.float().abs().max()
