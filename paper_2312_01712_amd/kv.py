@@ -135,6 +135,7 @@ class Step:
         self._c = _Step(R, T, table.shape[1], table.data_ptr(), kv_lens.data_ptr(), q_start.data_ptr(), slots.data_ptr(),
                         requests.data_ptr(), positions.data_ptr())
         self._ref, self._state = ctypes.byref(self._c), free_state.data_ptr()
+        self._held = (kv_lens, q_start, table, slots, requests, positions, free_state)  # what the addresses above belong to
 
     @classmethod
     def empty(cls, requests: int, max_tokens: int, table: torch.Tensor) -> "Step":
@@ -185,6 +186,7 @@ class KvCache:
         self.boxes = torch.zeros(n_pages, kv_heads, 2, head_dim, dtype=torch.bfloat16, device=device)
         self.device = self.pages.device.index
         self._c = _Cache(n_pages, kv_heads, head_dim, _DTYPES[dtype], self.pages.data_ptr(), self.boxes.data_ptr())
+        self._held = (self.pages, self.boxes)
         self._ref = ctypes.byref(self._c)
 
     def free_ring(self) -> Tuple[torch.Tensor, torch.Tensor]:
