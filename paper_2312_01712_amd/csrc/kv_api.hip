@@ -211,7 +211,7 @@ int ivfpq_kv_select(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, ivfpq_kv_ro
   rc = check_workspace(d_workspace, workspace_bytes, ivfpq_kv_select_workspace_bytes(c, s, heads), fn);
   if (rc) return rc;
   KvSelectArgs a = {};
-  a.boxes = c->boxes; a.q = static_cast<const uint16_t *>(q.data); a.table = s->table; a.q_start = s->q_start;
+  a.boxes = c->boxes; a.q = static_cast<const uint16_t *>(q.data); a.table = s->table;
   a.token_req = s->token_req; a.positions = s->positions; a.scores = static_cast<float *>(d_workspace); a.out = d_out;
   a.q_token = q.token_stride; a.q_head = q.head_stride; a.n_pages = c->n_pages; a.kv_heads = c->kv_heads;
   a.group = heads / c->kv_heads; a.requests = s->requests; a.tokens = s->max_tokens; a.width = s->table_width;

@@ -483,7 +483,7 @@ __device__ inline void clear_rest(const KvAttnArgs &a, int64_t wg, int64_t n_wg,
 // softmax state; what a workgroup has of a unit whose pages it does not have all goes to the
 // workspace, and kv_join_kernel adds up.  Where the table is narrow a workgroup has a whole unit instead.
 // Bound by reading the pages (decode: 16 rows or fewer share a page): one token of 520 001, 566 MB, 109 us (5.2 TB/s); 40
-// requests of 700 to 33 000, 361 MB, 91 us; 24 x 64 selected pages, 108 MB, 27 us; 334 tokens of 12 heads of 64 6.2 us, the
+// requests of 700 to 33 000, 361 MB, 91 us; 24 x 64 selected pages, 108 MB, 29 us; 334 tokens of 12 heads of 64 6.2 us, the
 // chain of its first trips to memory.
 template <int D, int DT, bool SEL>
 __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
@@ -939,7 +939,8 @@ Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D,
     const int64_t seen = ((int64_t)window + (max_new < tokens ? max_new : tokens)) / KV_PAGE + 2;
     if (seen < most) most = seen;
   }
-  const bool narrow = most <= WHOLE_PAGES;
+  // (64 selected pages of 24 tokens and 8 kv heads: 30 us whole, 32 in shares and joined)
+  const bool narrow = most <= WHOLE_PAGES || (n_select > 0 && most <= 64 && tokens * kv_heads >= 128);
   // Chunks: tiles of 256 rows where they fill the CUs (a page is unpacked by twice the wavefronts: 2048 tokens,
   // 32 heads, behind 8190: 349 us, 128 rows 380), of 128 otherwise, and of 64 where units are short, so that shares
   // cannot fill the chip instead (1700 tokens, 16 heads of their own keys, a window of 1000: 38 us, 128 rows 44).

@@ -44,7 +44,7 @@ struct KvAppendArgs {
 
 struct KvSelectArgs {
   const uint16_t *boxes, *q;
-  const int32_t *table, *q_start, *kv_lens, *token_req, *positions;
+  const int32_t *table, *token_req, *positions;
   float *scores;  // [tokens][kv_heads][score_width]
   int32_t *out;
   int64_t q_token, q_head, n_pages;

@@ -387,6 +387,19 @@ def test_attention_selected(kv, dtype, H, G, D):
     s.attend(H * G, selected=sel, window=90)
 
 
+@pytest.mark.parametrize("n", [20, 40, 64, 70])
+def test_attention_of_many_selections(kv, n):
+    """Lists short enough for a workgroup each and longer ones, of many tokens and heads."""
+    rng = np.random.default_rng(n)
+    s = Server(kv, rng, "bf16", 4, 64, 500, 6, 90)
+    s.fill([5000, 640, 0, 4200, 64, 2500])
+    s.fill([9, 4, 3, 7, 8, 5], max_tokens=37)
+    q, qn = rows(rng, "bf16", 37, 8, 64)
+    got = s.cache.select(q, s.step, n, sinks=2, recent=1).cpu().numpy().astype(np.int64)
+    assert np.array_equal(got, ref.select(s.ref, qn, 4, s.want, 500, n, 2, 1))
+    s.attend(8, selected=got)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_attention_of_large_scores(kv, dtype):
     """Scores of hundreds and thousands, of both signs: the running maximum moves by more than exponentials hold."""
