@@ -172,24 +172,26 @@ __device__ inline void page_values(const Page<D> &pg, const u32x4 *pf, f32x4 *o)
 }
 
 // The largest product of a page joins a row's maximum; what the row has so far shrinks with it.  first: position of the
-// page's first key; the row sees (low, high].  Products are compared unscaled (scale2 > 0): one multiply-add an exponential.
+// page's first key; the row sees (low, high], low >= -1.  Products are compared unscaled (scale2 > 0): one multiply-add an
+// exponential.  A maximum that grows by less than 2^LAZY is left: weights up to 2^LAZY lose nothing in either type, and most
+// pages of a long context go without the multiplications.
+constexpr float LAZY = 8.0f;
+
 template <int D>
 __device__ inline void page_maximum(f32x4 *s, Row<D> &r, int g, float scale2, bool masked, int first, int low, int high) {
   if (masked) {
+    const int from = low - first - g * 4, to = high - first - g * 4;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = first + tt * 16 + g * 4 + i;
-        s[tt][i] = j > low && j <= high ? s[tt][i] : -__builtin_inff();
-      }
+      for (int i = 0; i < 4; ++i) s[tt][i] = tt * 16 + i > from && tt * 16 + i <= to ? s[tt][i] : -__builtin_inff();
   }
   float top = s[0][0];
 #pragma unroll
   for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e >> 2][e & 3]);
-  const float m = fmaxf(r.m, row_max(top) * scale2);
-  if (__any(m > r.m)) {
-    const float f = m > r.m ? __builtin_amdgcn_exp2f(r.m - m) : 1.0f;
+  top = row_max(top) * scale2;
+  if (__any(top > r.m + LAZY)) {
+    const float m = fmaxf(r.m, top), f = m > r.m ? __builtin_amdgcn_exp2f(r.m - m) : 1.0f;
     r.l *= f;
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct)
@@ -394,11 +396,11 @@ __device__ inline Place place_of(const KvAttnArgs &a, const Unit &u, int rows, i
   const int i0 = u.tile * TR + min(in_tile & ~15, rows - 1), i1 = u.tile * TR + min(in_tile | 15, rows - 1);
   const int pos = u.pos0 + i / a.group, pos_a = u.pos0 + i0 / a.group, pos_b = u.pos0 + i1 / a.group;
   p.high = min(pos, u.kv - 1);
-  p.low = a.window > 0 ? pos - a.window : -1;
+  p.low = a.window > 0 ? max(pos - a.window, -1) : -1;
   p.clear_high = uniform(min(pos_a, u.kv - 1));
   p.any_high = uniform(min(pos_b, u.kv - 1));
-  p.clear_low = uniform(a.window > 0 ? pos_b - a.window : -1);
-  p.any_low = uniform(a.window > 0 ? pos_a - a.window : -1);
+  p.clear_low = uniform(a.window > 0 ? max(pos_b - a.window, -1) : -1);
+  p.any_low = uniform(a.window > 0 ? max(pos_a - a.window, -1) : -1);
   return p;
 }
 
