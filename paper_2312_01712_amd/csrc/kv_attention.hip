@@ -173,12 +173,12 @@ __device__ inline void page_values(const Page<D> &pg, const u32x4 *pf, f32x4 *o)
 
 // The largest product of a page joins a row's maximum; what the row has so far shrinks with it.  first: position of the
 // page's first key; the row sees (low, high], low >= -1.  Products are compared unscaled (scale2 > 0): one multiply-add an
-// exponential.  A maximum that grows by less than 2^LAZY is left: weights up to 2^LAZY lose nothing in either type, and most
-// pages of a long context go without the multiplications.
-constexpr float LAZY = 8.0f;
-
+// exponential.  slack: a maximum that grows by less (in powers of two) is left, and weights go up to 2^slack.  That
+// costs no bits, only that the largest weight is 1, which is exact; chunks take it (8: 333 us for 348, the
+// results 0.0023 off for 0.0019 in bf16), decoding, which waits for memory, does not.
 template <int D>
-__device__ inline void page_maximum(f32x4 *s, Row<D> &r, int g, float scale2, bool masked, int first, int low, int high) {
+__device__ inline void page_maximum(f32x4 *s, Row<D> &r, int g, float scale2, bool masked, int first, int low, int high,
+                                    float slack) {
   if (masked) {
     const int from = low - first - g * 4, to = high - first - g * 4;
 #pragma unroll
@@ -190,7 +190,7 @@ __device__ inline void page_maximum(f32x4 *s, Row<D> &r, int g, float scale2, bo
 #pragma unroll
   for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e >> 2][e & 3]);
   top = row_max(top) * scale2;
-  if (__any(top > r.m + LAZY)) {
+  if (__any(top > r.m + slack)) {
     const float m = fmaxf(r.m, top), f = m > r.m ? __builtin_amdgcn_exp2f(r.m - m) : 1.0f;
     r.l *= f;
 #pragma unroll
@@ -223,7 +223,7 @@ __device__ inline void page_step(const Page<D> &pg, const u32x4 *qf, Row<D> &r, 
   f32x4 s[4];
   u32x4 pf[2];
   page_scores<D, DT>(pg, qf, lane, s);
-  page_maximum<D>(s, r, lane >> 4, scale2, masked, first, low, high);
+  page_maximum<D>(s, r, lane >> 4, scale2, masked, first, low, high, 0.0f);
   page_weights<D, DT>(s, r, pf, scale2);
   page_values<D, DT>(pg, pf, r.o);
 }
@@ -676,8 +676,8 @@ __device__ inline void lds_barrier() {
 // Many rows of one kv head: a workgroup unpacks a page into LDS, one ahead of the one worked on (two
 // buffers, a barrier a page), and each of its wavefronts has NQ times 16 rows with their queries, weights
 // and results in registers.  A fragment read from LDS feeds NQ products.  Bound by the matrix units (35 % busy)
-// and the vector ones (50 %; an exponential takes 16 cycles): 2048 tokens of 32 heads behind 8190, 309 GFLOP, 349 us
-// (889 TFLOP/s; an 8192^3 library product reaches 1203).
+// and the vector ones (50 %; an exponential takes 16 cycles): 2048 tokens of 32 heads behind 8190, 309 GFLOP, 333 us
+// (929 TFLOP/s; an 8192^3 library product reaches 1203).
 template <int D, int DT, int WAVES, int NQ>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, WAVES * NQ == 4 ? 3 : 2))) void kv_rows_kernel(KvAttnArgs a) {
   constexpr int TR = WAVES * NQ * 16, C = D / 32, FRAGS = page_fragments<D>(), THREADS = 64 * WAVES;
@@ -793,7 +793,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, W
 #pragma unroll
         for (int k = 0; k < NQ; ++k) {
           const bool masked = first + KV_PAGE - 1 > p[k].clear_high || first <= p[k].clear_low;
-          page_maximum<D>(s[k], r[k], g, a.scale2, masked, first, p[k].low, p[k].high);
+          page_maximum<D>(s[k], r[k], g, a.scale2, masked, first, p[k].low, p[k].high, 8.0f);
         }
         read(4 * C, x[0]);
         __builtin_amdgcn_sched_barrier(0);
