@@ -269,9 +269,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a, int tile
 
 template <int D>
 static void append_of(const KvAppendArgs &a, int dtype, hipStream_t s) {
-  // few tokens: a wavefront for each, should they be runs of one; many: most are not the first of their run, and a
-  // workgroup without one costs as much as a quarter of one with (12 750 tokens: 34 us with 16 tokens a workgroup)
-  const int tile = a.tokens <= 2048 ? 4 : a.tokens <= 8192 ? 16 : 64;
+  // few tokens: a wavefront for each, should they be runs of one (48 tokens: 5.6 us, 16 a workgroup 14.9); many: most are not
+  // the first of their run, or there are workgroups enough (2000 of one prompt: 8.2 us, 4 a workgroup 17.2; 3000 runs
+  // of one: 41 and 43)
+  const int tile = a.tokens <= 512 ? 4 : 16;
   const dim3 grid((unsigned)((a.tokens + tile - 1) / tile), (unsigned)a.kv_heads);
   if (dtype == IVFPQ_KV_BF16) hipLaunchKernelGGL((kv_append_kernel<D, IVFPQ_KV_BF16>), grid, dim3(256), 0, s, a, tile);
   else hipLaunchKernelGGL((kv_append_kernel<D, IVFPQ_KV_FP16>), grid, dim3(256), 0, s, a, tile);

@@ -941,14 +941,18 @@ Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D,
     const int64_t seen = ((int64_t)window + (max_new < tokens ? max_new : tokens)) / KV_PAGE + 2;
     if (seen < most) most = seen;
   }
-  // (64 selected pages of 24 tokens and 8 kv heads: 30 us whole, 32 in shares and joined)
-  const bool narrow = most <= WHOLE_PAGES || (n_select > 0 && most <= 64 && tokens * kv_heads >= 128);
+  // 16 rows a tile up to 64 rows of a request and head (16 requests of 8001 tokens, 64 rows: 91 us, in a tile of the
+  // chunks' kernel 95; 64 rows of one of 32 000: 35 and 51; 128 rows go either way: 168 and 108, 49 and 56).
+  const bool few = n_select > 0 || rows <= 64;
+  // Whole units where they are short: 32 requests of 1900 tokens 19 us, in shares and joined 24, 4 requests 15 and 13, one of
+  // 334 7.7 and 11; up to twice as long where there are enough of them: 32 requests of 3900 30 us and 36, 4 requests 24 and 16.
+  const bool narrow = most <= WHOLE_PAGES || (few && most <= 2 * WHOLE_PAGES && tokens * kv_heads >= 128);
   // Chunks: tiles of 256 rows where they fill the CUs (a page is unpacked by twice the wavefronts: 2048 tokens,
-  // 32 heads, behind 8190: 349 us, 128 rows 380), of 128 otherwise, and of 64 where units are short, so that shares
-  // cannot fill the chip instead (1700 tokens, 16 heads of their own keys, a window of 1000: 38 us, 128 rows 44).
-  // 256 channels have no registers for more than 16 rows a wavefront.
+  // 32 heads, behind 8190: 331 us, 128 rows 379; 4 x 700 behind 2000: 162 and 172), of 128 otherwise, and of 64 where units
+  // are short, so that shares cannot fill the chip instead (1700 tokens, 16 heads of their own keys, a window of 1000:
+  // 38 us, 128 rows 44).  256 channels have no registers for more than 16 rows a wavefront.
   const int64_t all = tokens * group * kv_heads;
-  s.tile_rows = n_select > 0 || rows <= 64 ? 16 : D == 256 ? 128 : all >= 256 * 256 ? 256 : narrow && all < 512 * 128 ? 64 : 128;
+  s.tile_rows = few ? 16 : D == 256 ? 128 : all >= 256 * 256 ? 256 : narrow && all < 512 * 128 ? 64 : 128;
   const int64_t units = n_select > 0 ? tokens * kv_heads * ((group + 15) / 16)
                                      : (tokens * group / s.tile_rows + requests) * kv_heads;
   // whole units where they are short, or (chunks) where there are many; shares otherwise: as many workgroups as the
