@@ -5,7 +5,7 @@
 // byte: the box needs no atomics and does not depend on any order.  A lane has eight channels of four
 // consecutive tokens (16-byte loads); four lanes share a scale.  Bound by memory: 4 D bytes read
 // and 68 D / 64 written per token and head, plus 4 D if the rounded rows are wanted: 12 750 tokens of 8 heads of
-// 128, 119 MB, in 31 us (3.8 TB/s); 48 tokens in 5.5 us.  Sizes are compared as bits and rows are rounded as they lie, two
+// 128, 119 MB, in 31 us (3.8 TB/s); 48 tokens in 5.7 us.  Sizes are compared as bits and rows are rounded as they lie, two
 // values an instruction: unpacked to 32 bits first it took 18 vector instructions an element and 34 us.
 
 #include "kv_internal.h"
