@@ -98,7 +98,7 @@ def _rows(t: torch.Tensor, dtype, shape, device: int, what: str) -> _Rows:
     if t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(t.shape)} does not match {tuple(shape)}")
     ts, hs, cs = t.stride()
-    if cs != 1:
+    if cs != 1 and t.numel():  # (strides of nothing are arbitrary)
         raise ValueError(f"{what}: the channels must be contiguous, their stride is {cs}")
     return _Rows(t.data_ptr() or None, ts, hs)
 
