@@ -75,6 +75,8 @@ typedef struct {
   int64_t *slots;      /* [max_tokens]    page * 64 + place in the page, or -1               */
   int32_t *token_req;  /* [max_tokens]    request, or -1                                     */
   int32_t *positions;  /* [max_tokens]    position in the request, or -1                     */
+  int32_t *counts;     /* [2 * requests]  room in which ivfpq_kv_plan counts pages of ended requests, or NULL: every
+                          workgroup counts them then, which takes longer with many              */
 } ivfpq_kv_step;
 
 /* Page tables and slot maps of a step.
@@ -85,8 +87,12 @@ typedef struct {
  *   free_pages  [free_capacity] ring of the pages that nobody holds; free_state [3]: first taken
  *               index, first index behind them (both count up), and how many pages were missing.
  *               Pages are taken in the order of requests and positions, those of ended requests
- *               are put behind the others and can be taken from the next step on.
- *               free_state_out must not be free_state.
+ *               are put behind the others and can be taken from the next step on.  The ring needs
+ *               room for every page that it and the tables hold (n_pages of the cache is enough);
+ *               what it has no room for is dropped.  free_state_out must not be free_state.
+ * Where pages are missing, the table has -1, the tokens have slot -1 and count as held all the same; they are neither
+ * stored nor seen by attention, in later steps too.  Such a request gives back the pages that it has when it
+ * ends (entries below 0 are no pages); or the step is done again, from the same lengths and state, with fewer new tokens.
  * Written: table and free_pages in place (doing a step again from the same lengths and state
  * gives the same), the step's other arrays (kv_lens: 0 for an ended request) and free_state_out.  A step has to
  * fit: past + new <= 64 * table_width (what is beyond has slot -1 and is not counted as held), and the

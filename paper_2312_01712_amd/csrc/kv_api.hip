@@ -146,7 +146,7 @@ int ivfpq_kv_plan(const ivfpq_kv_step *s, const int32_t *past_lens, const int32_
   a.past = past_lens; a.fresh = new_lens; a.table = s->table; a.free_pages = free_pages; a.kv_lens = s->kv_lens;
   a.q_start = s->q_start; a.token_req = s->token_req; a.positions = s->positions; a.slots = s->slots; a.state = free_state;
   a.state_out = free_state_out; a.capacity = free_capacity; a.requests = s->requests; a.width = s->table_width;
-  a.max_tokens = s->max_tokens;
+  a.max_tokens = s->max_tokens; a.counts = s->counts;
   return launch_kv_plan(a, static_cast<hipStream_t>(stream));
 }
 

@@ -26,6 +26,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 struct KvPlanArgs {
   const int32_t *past, *fresh;
   int32_t *table, *free_pages, *kv_lens, *q_start, *token_req, *positions;
+  int32_t *counts;  // [requests] pages of ended requests, or null: every workgroup counts
+  int32_t *totals;  // [groups of 16 requests][3] new tokens, pages taken and given; behind the counts, or null
   int64_t *slots;
   const int64_t *state;
   int64_t *state_out, capacity;

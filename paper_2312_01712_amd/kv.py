@@ -38,7 +38,7 @@ class _Cache(ctypes.Structure):
 
 class _Step(ctypes.Structure):
     _fields_ = [("requests", _i32), ("max_tokens", _i32), ("table_width", _i32), ("table", _vp), ("kv_lens", _vp),
-                ("q_start", _vp), ("slots", _vp), ("token_req", _vp), ("positions", _vp)]
+                ("q_start", _vp), ("slots", _vp), ("token_req", _vp), ("positions", _vp), ("counts", _vp)]
 
 
 class _Rows(ctypes.Structure):
@@ -132,10 +132,11 @@ class Step:
         _dev(positions, torch.int32, (T,), dev, "positions")
         _dev(free_state, torch.int64, (3,), dev, "free_state")
         self.max_tokens = T
+        counts = torch.empty(2 * R, dtype=torch.int32, device=table.device)  # room for plan
         self._c = _Step(R, T, table.shape[1], table.data_ptr(), kv_lens.data_ptr(), q_start.data_ptr(), slots.data_ptr(),
-                        requests.data_ptr(), positions.data_ptr())
+                        requests.data_ptr(), positions.data_ptr(), counts.data_ptr() or None)
         self._ref, self._state = ctypes.byref(self._c), free_state.data_ptr()
-        self._held = (kv_lens, q_start, table, slots, requests, positions, free_state)  # what the addresses above belong to
+        self._held = (kv_lens, q_start, table, slots, requests, positions, free_state, counts)  # what the addresses above belong to
 
     @classmethod
     def empty(cls, requests: int, max_tokens: int, table: torch.Tensor) -> "Step":
@@ -149,7 +150,8 @@ class Step:
 def plan(past_lens: torch.Tensor, new_lens: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
          free_state: torch.Tensor, max_tokens: Optional[int] = None, out: Optional[Step] = None) -> Step:
     """Page tables and slot maps of a step (`ivfpq_kv_plan`).  past_lens, new_lens [R] int32 (new < 0: the request
-    ends); table [R][W] and free_pages [capacity] int32 are updated in place; free_state [3] int64."""
+    ends); table [R][W] and free_pages [capacity] int32 are updated in place; free_state [3] int64.
+    `free_state[2]` of the result says how many pages were missing: their tokens are not stored."""
     if out is None:
         if max_tokens is None:
             raise ValueError("plan: max_tokens, the most new tokens of the step, is needed without out")
