@@ -958,15 +958,19 @@ Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D,
   // whole units where they are short, or (chunks) where there are many; shares otherwise: as many workgroups as the
   // chip holds at a time, four pages each at least
   const int fill = s.tile_rows == 16 ? 512 : s.tile_rows == 128 && D < 256 ? 512 : 256;
+  const bool units_fit = narrow || (s.tile_rows > 16 && units >= 1024);
   // (and where their pages cannot be counted in 31 bits, whatever max_new promises)
   const int64_t surely = n_select > 0 ? n_select : window > 0 ? (window + tokens) / KV_PAGE + 2 : width;
-  s.whole = narrow || (s.tile_rows > 16 && units >= 1024) || units * (n_select > 0 || surely < width ? surely : width) > 0x7fffffff;
-  s.n_wg = s.whole ? (int)units : units * most / 4 >= fill ? fill : (int)(units * most / 4 + 1);
+  s.whole = units_fit || units * (n_select > 0 || surely < width ? surely : width) > 0x7fffffff;
+  const int shares = units * most / 4 >= fill ? fill : (int)(units * most / 4 + 1);
+  s.n_wg = s.whole ? (int)units : shares;
   if (s.n_wg < 1) s.n_wg = 1;
+  // Room for shares also where only the 31 bits forbid them: a window may lift that, and what is asked for without one has
+  // to be enough.
   s.prefix = up256((size_t)(requests + 1) * 4);
-  s.borders = s.whole ? 0 : up256((size_t)s.n_wg * BORDER_INTS * 4);
-  s.ml = s.whole ? 0 : up256((size_t)s.n_wg * 2 * s.tile_rows * 2 * 4);
-  s.o = s.whole ? 0 : up256((size_t)s.n_wg * 2 * s.tile_rows * D * 4);
+  s.borders = units_fit ? 0 : up256((size_t)shares * BORDER_INTS * 4);
+  s.ml = units_fit ? 0 : up256((size_t)shares * 2 * s.tile_rows * 2 * 4);
+  s.o = units_fit ? 0 : up256((size_t)shares * 2 * s.tile_rows * D * 4);
   return s;
 }
 

@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_kv_gpu import Server, kv  # noqa: F401
+import kv_reference as ref
+from test_kv_gpu import Server, compare, dev, kv, rows  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -22,3 +23,20 @@ def test_a_step_without_tokens(kv):
         out, lse = s.cache.attention(q, s.step, max_new=1)
         assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
     assert torch.equal(s.cache.pages, before)
+
+
+def test_a_window_over_a_very_wide_table(kv):
+    """So many columns that pages are counted in 31 bits only with the window: the calls' own workspace is enough."""
+    rng = np.random.default_rng(1)
+    R, H, G = 256, 8, 8
+    s = Server(kv, rng, "bf16", H, 64, 2 * R, R, 2)
+    s.fill(rng.integers(1, 100, R))
+    s.fill([1] * R)
+    wide = torch.full((R, 1 << 20), -1, dtype=torch.int32, device="cuda")
+    wide[:, :2] = s.d_table
+    t = s.step
+    step = kv.Step(t.kv_lens, t.q_start, wide, t.slots, t.requests, t.positions, t.free_state)
+    q, qn = rows(rng, "bf16", R, H * G, 64)
+    for window in (0, 50, 5000):
+        out, lse = s.cache.attention(q, step, window=window, max_new=1)
+        compare(out, lse, *ref.attention(s.ref, qn, H, s.want, 2 * R, 64 ** -0.5, window), 64, False)
