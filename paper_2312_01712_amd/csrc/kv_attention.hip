@@ -1,6 +1,6 @@
 // Attention of a step's new tokens over the paged 4-bit cache, all pages or selected ones.
 //
-// The running form of the softmax: with s_j = scale log2(e) q . k_j, a row keeps m = max s_j,
+// The running form of the softmax: with s_j = scale log2(e) q . k_j, a row keeps m = max s_j (or a number near it),
 // l = sum 2^(s_j - m) and o = sum 2^(s_j - m) v_j and multiplies l and o by 2^(m_old - m_new) when m
 // grows; parts of the keys joined the same way.  Sums and statistics are in 32 bits, weights are
 // rounded to the cache's type for the second product (as the values are: both factors exact or
@@ -174,9 +174,12 @@ __device__ inline void page_values(const Page<D> &pg, const u32x4 *pf, f32x4 *o)
 // The largest product of a page joins a row's maximum; what the row has so far shrinks with it.  first: position of the
 // page's first key; the row sees (low, high], low >= -1.  Products are compared unscaled (scale2 > 0): one multiply-add an
 // exponential.  slack: a maximum that grows by less (in powers of two) is left, and weights go up to 2^slack.  That
-// costs no bits, only that the largest weight is 1, which is exact; chunks take it (8: 333 us for 348, the
-// results 0.0023 off for 0.0019 in bf16), decoding, which waits for memory, does not.
-template <int D>
+// costs accuracy: without it the largest weight is a power of two, which its rounding leaves alone.  Chunks take it (8: 333 us
+// for 348, the results 0.0023 off for 0.0019 in bf16), decoding, which waits for memory, does not.
+// In fp16, whose smallest step is 2^-24, m is the maximum less 15 - slack: weights go up to 2^15, and one loses 2^-40 of the
+// largest (with a slack 2^-32) to that step instead of 2^-25, which many small ones together would miss.  l and o carry
+// the same factor, so that nothing else knows of it.
+template <int D, int DT>
 __device__ inline void page_maximum(f32x4 *s, Row<D> &r, int g, float scale2, bool masked, int first, int low, int high,
                                     float slack) {
   if (masked) {
@@ -189,7 +192,8 @@ __device__ inline void page_maximum(f32x4 *s, Row<D> &r, int g, float scale2, bo
   float top = s[0][0];
 #pragma unroll
   for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e >> 2][e & 3]);
-  top = row_max(top) * scale2;
+  const float lift = DT == IVFPQ_KV_FP16 ? 15.0f - slack : 0.0f;
+  top = row_max(top) * scale2 - lift;
   if (__any(top > r.m + slack)) {
     const float m = fmaxf(r.m, top), f = m > r.m ? __builtin_amdgcn_exp2f(r.m - m) : 1.0f;
     r.l *= f;
@@ -223,7 +227,7 @@ __device__ inline void page_step(const Page<D> &pg, const u32x4 *qf, Row<D> &r, 
   f32x4 s[4];
   u32x4 pf[2];
   page_scores<D, DT>(pg, qf, lane, s);
-  page_maximum<D>(s, r, lane >> 4, scale2, masked, first, low, high, 0.0f);
+  page_maximum<D, DT>(s, r, lane >> 4, scale2, masked, first, low, high, 0.0f);
   page_weights<D, DT>(s, r, pf, scale2);
   page_values<D, DT>(pg, pf, r.o);
 }
@@ -793,7 +797,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, W
 #pragma unroll
         for (int k = 0; k < NQ; ++k) {
           const bool masked = first + KV_PAGE - 1 > p[k].clear_high || first <= p[k].clear_low;
-          page_maximum<D>(s[k], r[k], g, a.scale2, masked, first, p[k].low, p[k].high, 8.0f);
+          page_maximum<D, DT>(s[k], r[k], g, a.scale2, masked, first, p[k].low, p[k].high, 8.0f);
         }
         read(4 * C, x[0]);
         __builtin_amdgcn_sched_barrier(0);

@@ -40,3 +40,34 @@ def test_a_window_over_a_very_wide_table(kv):
     for window in (0, 50, 5000):
         out, lse = s.cache.attention(q, step, window=window, max_new=1)
         compare(out, lse, *ref.attention(s.ref, qn, H, s.want, 2 * R, 64 ** -0.5, window), 64, False)
+
+
+@pytest.mark.parametrize("W,max_new,new", [(12, 1, 1), (400, 1, 1), (12, 70, 70), (400, 70, 70), (12, 300, 300)])
+@pytest.mark.parametrize("dtype,gap", [("fp16", 14.0), ("fp16", 17.5), ("bf16", 17.5)])
+def test_a_key_far_ahead_of_many(kv, dtype, gap, W, max_new, new):
+    """One key's score is `gap` above the others', its value is 0: the result is the others' alone, each with a weight below
+    half the smallest step of fp16.  Weights are rounded once, u of each; fp16 weights are held times 2^7 at least, so that what
+    its smallest step loses of one is 2^-32 of the largest at most."""
+    rng = np.random.default_rng(int(gap) + new)
+    s = Server(kv, rng, dtype, 1, 64, 14, 1, W)
+    s.gain[:] = 0.05
+
+    def first_ahead(k, v):
+        k[:, 0, 0], v[:] = 0.0, (1 + v.abs()) * 40
+        k[0, 0, 0], v[0] = 4.0, 0.0
+
+    def others(k, v):
+        k[:, 0, 0], v[:] = 0.0, (1 + v.abs()) * 40
+    s.fill([500], edit=first_ahead)
+    s.fill([new], edit=others)
+    q, _ = rows(rng, dtype, new, 2, 64)
+    q[:, :, 0] = gap / 4
+    qn = q.double().cpu().numpy()
+    out, lse = s.cache.attention(q, s.step, scale=1.0, max_new=max_new)
+    w_out, w_lse, mass, reach, size = ref.attention(s.ref, qn, 1, s.want, 14, 1.0)
+    off, off_lse = ref.bounds(w_out, w_lse, mass, reach, size, 64, dtype == "fp16")
+    if dtype == "fp16":
+        off = off - 2.0 ** -25 * reach + 2.0 ** -32 * reach
+    assert (np.abs(out.double().cpu().numpy() - w_out) <= off).all()
+    assert (np.abs(lse.double().cpu().numpy() - w_lse) <= off_lse).all()
+    assert (w_out > 4 * off).all()
