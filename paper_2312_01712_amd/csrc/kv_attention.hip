@@ -1051,6 +1051,10 @@ size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, in
 int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s) {
   const Shape sh = shape_of(a.tokens, a.requests, a.kv_heads, a.group, D, max_new, a.window, a.selected ? a.n_select : 0,
                             a.width);
+  if (!launch_fits(sh.n_wg, sh.tile_rows == 256 || (sh.tile_rows == 128 && D == 256) ? 512 : 256)) {
+    set_error("kv_attention: %d workgroups are too many for one launch", sh.n_wg);
+    return IVFPQ_ERR_UNSUPPORTED;
+  }
   a.n_wg = sh.n_wg;
   a.whole = sh.whole;
   a.prefix = reinterpret_cast<int32_t *>(workspace);

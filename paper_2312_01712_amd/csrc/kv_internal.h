@@ -78,6 +78,9 @@ size_t kv_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, in
                               int n_select, int64_t width);
 int launch_kv_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s);
 
+// A launch may have fewer than 2^32 threads along its grid's first dimension.
+inline bool launch_fits(int64_t workgroups, int64_t threads) { return workgroups * threads < (int64_t)1 << 32; }
+
 #define KV_HIP_TRY(expr)                                \
   do {                                                  \
     hipError_t _e = (expr);                             \

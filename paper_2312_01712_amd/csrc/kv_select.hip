@@ -393,18 +393,25 @@ void score_of(const KvSelectArgs &a, int dtype, dim3 grid, int GP, int tpt, int 
 }  // namespace
 
 int launch_kv_select(const KvSelectArgs &a, int D, int dtype, hipStream_t s) {
-  if (a.requests > 0 && a.width > a.n_select) {
-    int GP = 1;
-    while (GP < a.group && GP < 16) GP <<= 1;
-    // one token a tile where a request has one (a tile would have its requests' pages one after the other: 61 requests of
-    // 20 000 tokens 25.8 us, four tokens a tile 27.7)
-    const int tpt = a.tokens <= a.requests ? 1 : 16 / GP;
-    const int64_t tiles = (a.tokens + tpt - 1) / tpt;
-    // pages of a workgroup: two turns of its wavefronts (one token of 262 001: 7.5 us, four turns 10.4; 61 ragged requests 22 for
-    // both), more where that would be a great many workgroups
-    int64_t chunk = 2 * SCORE_PAGES;
-    while (chunk < 1024 && tiles * a.kv_heads * ((a.width + chunk - 1) / chunk) > 16384) chunk *= 2;
-    const dim3 grid((unsigned)(tiles * a.kv_heads * ((a.width + chunk - 1) / chunk)));
+  const bool scored = a.requests > 0 && a.width > a.n_select;
+  int GP = 1;
+  while (GP < a.group && GP < 16) GP <<= 1;
+  // one token a tile where a request has one (a tile would have its requests' pages one after the other: 61 requests of
+  // 20 000 tokens 25.8 us, four tokens a tile 27.7)
+  const int tpt = a.tokens <= a.requests ? 1 : 16 / GP;
+  const int64_t tiles = (a.tokens + tpt - 1) / tpt;
+  // pages of a workgroup: two turns of its wavefronts (one token of 262 001: 7.5 us, four turns 10.4; 61 ragged requests 22 for
+  // both), more where that would be a great many workgroups
+  int64_t chunk = 2 * SCORE_PAGES;
+  while (chunk < 1024 && tiles * a.kv_heads * ((a.width + chunk - 1) / chunk) > 16384) chunk *= 2;
+  const int64_t score_wg = tiles * a.kv_heads * ((a.width + chunk - 1) / chunk);
+  const int pick_threads = a.width <= 1024 ? 256 : 1024;
+  if ((scored && !launch_fits(score_wg, 256)) || !launch_fits(a.tokens, pick_threads)) {
+    set_error("kv_select: %d tokens of %d kv heads and %d columns are too many for one launch", a.tokens, a.kv_heads, a.width);
+    return IVFPQ_ERR_UNSUPPORTED;
+  }
+  if (scored) {
+    const dim3 grid((unsigned)score_wg);
     switch (D) {
       case 64: score_of<64>(a, dtype, grid, GP, tpt, (int)chunk, s); break;
       case 96: score_of<96>(a, dtype, grid, GP, tpt, (int)chunk, s); break;
@@ -416,9 +423,9 @@ int launch_kv_select(const KvSelectArgs &a, int D, int dtype, hipStream_t s) {
   // threads by the columns that their registers hold (700 columns: 25.4 us both launches, 1024 threads 26.2; 3200: 21.0, 256
   // threads 25.3)
   const dim3 grid((unsigned)a.tokens, (unsigned)a.kv_heads);
-  if (a.width <= 1024) hipLaunchKernelGGL((kv_pick_kernel<256, 1>), grid, dim3(256), 0, s, a);
-  else if (a.width <= 4096) hipLaunchKernelGGL((kv_pick_kernel<1024, 1>), grid, dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((kv_pick_kernel<1024, 4>), grid, dim3(1024), 0, s, a);
+  if (a.width <= 1024) hipLaunchKernelGGL((kv_pick_kernel<256, 1>), grid, dim3(pick_threads), 0, s, a);
+  else if (a.width <= 4096) hipLaunchKernelGGL((kv_pick_kernel<1024, 1>), grid, dim3(pick_threads), 0, s, a);
+  else hipLaunchKernelGGL((kv_pick_kernel<1024, 4>), grid, dim3(pick_threads), 0, s, a);
   KV_HIP_TRY(hipGetLastError());
   return IVFPQ_OK;
 }

@@ -30,3 +30,26 @@ def test_workspace_without_a_window_is_enough_at_random():
         max_new, window = wide(1, T + 1), wide(1, 1 << 27)
         free = workspace(T, R, W, H, G, D, max_new)
         assert free >= workspace(T, R, W, H, G, D, max_new, window) > 0, (T, R, W, H, G, D, max_new, window)
+
+
+@pytest.mark.parametrize("T,R,W,H,G,D,max_new,n_select", [
+    (1 << 21, 1 << 16, 8, 8, 1, 128, 1, 4),      # selected pages: 2^24 units of 256 threads
+    (1 << 24, 1 << 16, 8, 1, 16, 64, 1, 4),
+    (1 << 24, 1, 8, 16, 1, 64, 1, 0),            # a tile of 16 rows each
+    (1 << 24, 1 << 16, 8, 130, 1, 64, 4096, 0),  # 256 rows, 512 threads
+    (1 << 22, 1 << 16, 8, 260, 1, 256, 4096, 0)])  # 128 rows, 512 threads
+def test_attention_refuses_launches_of_2_32_threads(T, R, W, H, G, D, max_new, n_select):
+    a = attention(heads=H * G, max_new=max_new, n_select=n_select, selected=P if n_select else None)
+    c, s = cache(kv_heads=H, head_dim=D), step(max_tokens=T, requests=R, table_width=W)
+    rc = kv._lib().ivfpq_kv_attention(ctypes.byref(c), ctypes.byref(s), ctypes.byref(a), 0x10000, 1 << 50, None)
+    assert rc == binding.ERR_UNSUPPORTED and "one launch" in binding.last_error()
+
+
+@pytest.mark.parametrize("T,R,W,H,G", [(1 << 24, 1 << 16, 8, 1, 1),     # 2^24 workgroups pick, of 256 threads
+                                       (1 << 22, 1 << 16, 2000, 1, 1),  # 2^22 of 1024
+                                       (1 << 21, 1 << 16, 8, 128, 16),  # scores: a workgroup a token and head
+                                       (1 << 20, 1, 20000, 8, 8)])
+def test_select_refuses_launches_of_2_32_threads(T, R, W, H, G):
+    c, s = cache(kv_heads=H), step(max_tokens=T, requests=R, table_width=W)
+    rc = kv._lib().ivfpq_kv_select(ctypes.byref(c), ctypes.byref(s), rows(), H * G, 4, 1, 1, P, 0x10000, 1 << 60, None)
+    assert rc == binding.ERR_UNSUPPORTED and "one launch" in binding.last_error()
