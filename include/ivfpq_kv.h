@@ -142,7 +142,7 @@ typedef struct {
   int32_t window;          /* 0: none                                                         */
   const int32_t *selected; /* device [max_tokens][kv_heads][n_select], or NULL                */
   int32_t n_select;
-  void *out;               /* device rows of the cache's type, aligned and strided as q       */
+  void *out;               /* device rows of the cache's type, aligned and strided as q; they must not overlap */
   int64_t out_token_stride, out_head_stride;
   float *lse;              /* device [max_tokens][heads], or NULL                             */
 } ivfpq_kv_attention_args;

@@ -77,6 +77,21 @@ int check_rows(const void *data, int64_t token_stride, int64_t head_stride, int6
   return IVFPQ_OK;
 }
 
+// Whether two rows of D elements share one.
+bool rows_meet(int64_t token_stride, int64_t head_stride, int64_t tokens, int64_t heads, int D) {
+  typedef __int128 wide;  // products of strides and extents
+  auto size = [](wide x) { return x < 0 ? -x : x; };
+  const wide ts = tokens > 1 ? size(token_stride) : 0, hs = heads > 1 ? size(head_stride) : 0;
+  if ((tokens > 1 && ts < D) || (heads > 1 && hs < D)) return true;
+  if (tokens < 2 || heads < 2 || ts >= (heads - 1) * hs + D || hs >= (tokens - 1) * ts + D) return false;
+  // neither lies within the other: for every distance of heads the tokens that come nearest
+  for (int64_t h = 1; h < heads; ++h) {
+    const wide t = h * hs / ts;
+    if ((t < tokens && h * hs - t * ts < D) || (t + 1 < tokens && (t + 1) * ts - h * hs < D)) return true;
+  }
+  return false;
+}
+
 int check_heads(const ivfpq_kv_cache *c, int32_t heads, const char *fn) {
   if (heads < c->kv_heads || heads % c->kv_heads || heads / c->kv_heads > 1024) {
     set_error("%s: heads = %d must be a multiple of kv_heads = %d, 1024 times that at most", fn, heads, c->kv_heads);
@@ -239,6 +254,7 @@ int ivfpq_kv_attention(const ivfpq_kv_cache *c, const ivfpq_kv_step *s, const iv
   if (rc) return rc;
   rc = check_rows(x->out, x->out_token_stride, x->out_head_stride, s->max_tokens, x->heads, "out", fn);
   if (rc) return rc;
+  if (rows_meet(x->out_token_stride, x->out_head_stride, s->max_tokens, x->heads, c->head_dim)) return invalid(fn, "rows of out overlap");
   const int group = x->heads / c->kv_heads;
   rc = check_workspace(d_workspace, workspace_bytes,
                        kv_attention_workspace(s->max_tokens, s->requests, c->kv_heads, group, c->head_dim, x->max_new,

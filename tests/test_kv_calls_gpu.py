@@ -71,3 +71,20 @@ def test_a_key_far_ahead_of_many(kv, dtype, gap, W, max_new, new):
     assert (np.abs(out.double().cpu().numpy() - w_out) <= off).all()
     assert (np.abs(lse.double().cpu().numpy() - w_lse) <= off_lse).all()
     assert (w_out > 4 * off).all()
+
+
+def test_results_into_rows_that_overlap_are_refused(kv):
+    from paper_2312_01712_amd.binding import ERR_INVALID_ARGUMENT, IvfpqError
+    s = Server(kv, np.random.default_rng(2), "bf16", 2, 64, 6, 2, 3)
+    s.fill([5, 3])
+    q, _ = rows(s.rng, "bf16", 8, 4, 64)
+    for out in (torch.empty(1, 4, 64, dtype=torch.bfloat16, device="cuda").expand(8, 4, 64),
+                torch.empty(8, 1, 64, dtype=torch.bfloat16, device="cuda").expand(8, 4, 64)):
+        with pytest.raises(IvfpqError) as e:
+            s.cache.attention(q, s.step, out=out)
+        assert e.value.status == ERR_INVALID_ARGUMENT
+    # rows between each other's, heads outside
+    out = torch.empty(4, 8, 64 + 8, dtype=torch.bfloat16, device="cuda").transpose(0, 1)[..., :64]
+    got, lse = s.cache.attention(q, s.step, out=out)
+    want = ref.attention(s.ref, q.double().cpu().numpy(), 2, s.want, 6, 64 ** -0.5)
+    compare(got, lse, *want, 64, False)

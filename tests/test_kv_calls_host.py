@@ -39,7 +39,8 @@ def test_workspace_without_a_window_is_enough_at_random():
     (1 << 24, 1 << 16, 8, 130, 1, 64, 4096, 0),  # 256 rows, 512 threads
     (1 << 22, 1 << 16, 8, 260, 1, 256, 4096, 0)])  # 128 rows, 512 threads
 def test_attention_refuses_launches_of_2_32_threads(T, R, W, H, G, D, max_new, n_select):
-    a = attention(heads=H * G, max_new=max_new, n_select=n_select, selected=P if n_select else None)
+    a = attention(heads=H * G, max_new=max_new, n_select=n_select, selected=P if n_select else None, out_token_stride=H * G * D,
+                  out_head_stride=D)
     c, s = cache(kv_heads=H, head_dim=D), step(max_tokens=T, requests=R, table_width=W)
     rc = kv._lib().ivfpq_kv_attention(ctypes.byref(c), ctypes.byref(s), ctypes.byref(a), 0x10000, 1 << 50, None)
     assert rc == binding.ERR_UNSUPPORTED and "one launch" in binding.last_error()
@@ -53,3 +54,22 @@ def test_select_refuses_launches_of_2_32_threads(T, R, W, H, G):
     c, s = cache(kv_heads=H), step(max_tokens=T, requests=R, table_width=W)
     rc = kv._lib().ivfpq_kv_select(ctypes.byref(c), ctypes.byref(s), rows(), H * G, 4, 1, 1, P, 0x10000, 1 << 60, None)
     assert rc == binding.ERR_UNSUPPORTED and "one launch" in binding.last_error()
+
+
+@pytest.mark.parametrize("T,heads,D,token,head,meet", [
+    (3, 8, 128, 0, 128, True), (3, 8, 128, 1024, 0, True), (3, 8, 128, 1016, 128, True), (3, 8, 128, 1024, 120, True),
+    (3, 8, 128, 128, 128, True), (1, 8, 128, 0, 120, True), (2, 1, 128, 64, 0, True), (3, 8, 128, -1016, 128, True),
+    (3, 8, 64, 192, 192 * 2, True), (3, 8, 64, 168, 256, False), (3, 8, 64, 168, 200, True),
+    (3, 8, 128, 1024, 128, False), (3, 8, 128, 128, 384, False), (3, 8, 128, -1024, 128, False), (1, 8, 128, 0, 128, False),
+    (1, 1, 128, 0, 0, False), (2, 1, 128, 128, 0, False), (5, 8, 128, 1 << 60, 1 << 61, True), (2, 8, 128, 1 << 60, 1 << 61, False), (3, 8, 64, 1 << 62, 64, False)])
+def test_rows_of_results_must_not_overlap(T, heads, D, token, head, meet):
+    """Refused before the workspace is looked at; what does not overlap gets that far.  The expectations are those of all
+    addresses written out."""
+    at = [t * token + h * head for t in range(T) for h in range(heads)]
+    at.sort()
+    assert meet == any(b - a < D for a, b in zip(at, at[1:]))
+    a = attention(heads=heads, out_token_stride=token, out_head_stride=head)
+    rc = kv._lib().ivfpq_kv_attention(ctypes.byref(cache(kv_heads=1, head_dim=D)), ctypes.byref(step(max_tokens=T)), ctypes.byref(a),
+                                      None, 0, None)
+    assert rc == (binding.ERR_INVALID_ARGUMENT if meet else binding.ERR_WORKSPACE)
+    assert ("overlap" in binding.last_error()) == meet
