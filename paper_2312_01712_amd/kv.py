@@ -109,7 +109,16 @@ def _heads_of(q: torch.Tensor) -> int:
     return q.shape[1]
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
+def _launch(device: int, call, *args) -> None:
+    """`call` with the stream that is current on the tensors' device, which is made the current one: the library launches there."""
+    if _current_device() == device:
+        _check(call(*args, _raw_stream(device)))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, _raw_stream(device)))
 
 
 class Step:
@@ -164,9 +173,9 @@ def plan(past_lens: torch.Tensor, new_lens: torch.Tensor, table: torch.Tensor, f
     if _ptr(table, torch.int32, (R, c.table_width), dev, "table") != (c.table or 0):
         raise ValueError("plan: out was made for another table")
     ring = _ptr(free_pages, torch.int32, free_pages.shape[:1], dev, "free_pages")
-    _check(_lib().ivfpq_kv_plan(out._ref, _ptr(past_lens, torch.int32, (R,), dev, "past_lens"),
-                                _ptr(new_lens, torch.int32, (R,), dev, "new_lens"), ring, free_pages.shape[0],
-                                _ptr(free_state, torch.int64, (3,), dev, "free_state"), out._state, _raw_stream(dev)))
+    _launch(dev, _lib().ivfpq_kv_plan, out._ref, _ptr(past_lens, torch.int32, (R,), dev, "past_lens"),
+            _ptr(new_lens, torch.int32, (R,), dev, "new_lens"), ring, free_pages.shape[0],
+            _ptr(free_state, torch.int64, (3,), dev, "free_state"), out._state)
     return out
 
 
@@ -208,7 +217,7 @@ class KvCache:
         to_k = to_v = None
         if rounded is not None:
             to_k, to_v = _ptr(rounded[0], dtype, shape, dev, "rounded k"), _ptr(rounded[1], dtype, shape, dev, "rounded v")
-        _check(_lib().ivfpq_kv_append(self._ref, kr, vr, at, shape[0], to_k, to_v, _raw_stream(dev)))
+        _launch(dev, _lib().ivfpq_kv_append, self._ref, kr, vr, at, shape[0], to_k, to_v)
 
     def _step(self, step: Step):
         if step._checked != self.device:
@@ -232,8 +241,8 @@ class KvCache:
         to = _ptr(out, torch.int32, (T, self.kv_heads, max(n_pages, 0)), dev, "out")
         ws = self.select_workspace(step, heads) if workspace is None else workspace
         size = ws.shape[0]
-        _check(_lib().ivfpq_kv_select(self._ref, self._step(step), qr, heads, n_pages, sinks, recent, to,
-                                      _ptr(ws, torch.uint8, (size,), dev, "workspace"), size, _raw_stream(dev)))
+        _launch(dev, _lib().ivfpq_kv_select, self._ref, self._step(step), qr, heads, n_pages, sinks, recent, to,
+                _ptr(ws, torch.uint8, (size,), dev, "workspace"), size)
         return out
 
     def attention_workspace(self, step: Step, heads: int, max_new: Optional[int] = None, n_select: int = 0) -> torch.Tensor:
@@ -268,6 +277,6 @@ class KvCache:
         size = ws.shape[0]
         args = _Attention(qr, heads, max_new, self.head_dim ** -0.5 if scale is None else scale, window, lists, n_select,
                           to.data, to.token_stride, to.head_stride, to_lse)
-        _check(_lib().ivfpq_kv_attention(self._ref, self._step(step), ctypes.byref(args),
-                                         _ptr(ws, torch.uint8, (size,), dev, "workspace"), size, _raw_stream(dev)))
+        _launch(dev, _lib().ivfpq_kv_attention, self._ref, self._step(step), ctypes.byref(args),
+                _ptr(ws, torch.uint8, (size,), dev, "workspace"), size)
         return out, lse

@@ -88,3 +88,16 @@ def test_results_into_rows_that_overlap_are_refused(kv):
     got, lse = s.cache.attention(q, s.step, out=out)
     want = ref.attention(s.ref, q.double().cpu().numpy(), 2, s.want, 6, 64 ** -0.5)
     compare(got, lse, *want, 64, False)
+
+
+def test_every_call_makes_its_device_the_current_one(kv, monkeypatch):
+    entered, real = [], torch.cuda.device
+    s = Server(kv, np.random.default_rng(3), "bf16", 2, 64, 6, 2, 3)
+    monkeypatch.setattr(kv, "_current_device", lambda: 1)  # as if another one were
+    monkeypatch.setattr(torch.cuda, "device", lambda index: entered.append(index) or real(index))
+    T = s.plan([70, 9])
+    q, _ = rows(s.rng, "bf16", T, 4, 64)
+    s.cache.append(q[:, :2], q[:, 2:], s.step.slots)
+    s.cache.select(q, s.step, 2)
+    s.cache.attention(q, s.step)
+    assert entered == [0] * 4

@@ -73,3 +73,29 @@ def test_rows_of_results_must_not_overlap(T, heads, D, token, head, meet):
                                       None, 0, None)
     assert rc == (binding.ERR_INVALID_ARGUMENT if meet else binding.ERR_WORKSPACE)
     assert ("overlap" in binding.last_error()) == meet
+
+
+def test_calls_go_to_the_device_of_their_tensors(monkeypatch):
+    """Another device is current: the tensors' one is while the library is called, with its stream."""
+    current, log = [1], []
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.was, current[0] = current[0], self.index
+
+        def __exit__(self, *_):
+            current[0] = self.was
+
+    monkeypatch.setattr(kv, "_current_device", lambda: current[0])
+    monkeypatch.setattr(kv.torch.cuda, "device", Device)
+    monkeypatch.setattr(kv, "_raw_stream", lambda device: 0x100 + device)
+
+    def call(*args):
+        log.append((current[0], args))
+        return binding.OK
+    kv._launch(0, call, 7, 8)
+    kv._launch(1, call, 9)
+    assert log == [(0, (7, 8, 0x100)), (1, (9, 0x101))] and current == [1]
