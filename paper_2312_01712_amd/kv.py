@@ -103,6 +103,13 @@ def _rows(t: torch.Tensor, dtype, shape, device: int, what: str) -> _Rows:
     return _Rows(t.data_ptr() or None, ts, hs)
 
 
+def _int32(x: int, what: str) -> int:
+    """A number that the library's 32 bits hold; ctypes would drop what is above them."""
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{what} = {x} does not fit 32 bits")
+    return x
+
+
 def _heads_of(q: torch.Tensor) -> int:
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q: expected a tensor [tokens][heads][head_dim]")
@@ -186,7 +193,7 @@ class KvCache:
     def __init__(self, n_pages: int, kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16, device=None):
         if dtype not in _DTYPES:
             raise ValueError(f"dtype must be torch.bfloat16 or torch.float16, not {dtype}")
-        size = _lib().ivfpq_kv_page_bytes(kv_heads, head_dim)
+        size = _lib().ivfpq_kv_page_bytes(_int32(kv_heads, "kv_heads"), _int32(head_dim, "head_dim"))
         if size == 0:
             raise ValueError(f"kv_heads = {kv_heads} outside [1, 1024] or head_dim = {head_dim} not 64, 96, 128 or 256")
         if not 1 <= n_pages <= 1 << 25:
@@ -236,9 +243,11 @@ class KvCache:
         (`ivfpq_kv_select`): [T][kv_heads][n_pages] int32.  q [T][heads][head_dim]."""
         T, heads, dev = step.max_tokens, _heads_of(q), self.device
         qr = _rows(q, self.dtype, (T, heads, self.head_dim), dev, "q")
+        _int32(n_pages, "n_pages")
         if out is None:
             out = torch.empty((T, self.kv_heads, max(n_pages, 0)), dtype=torch.int32, device=q.device)
         to = _ptr(out, torch.int32, (T, self.kv_heads, max(n_pages, 0)), dev, "out")
+        sinks, recent = _int32(sinks, "sinks"), _int32(recent, "recent")
         ws = self.select_workspace(step, heads) if workspace is None else workspace
         size = ws.shape[0]
         _launch(dev, _lib().ivfpq_kv_select, self._ref, self._step(step), qr, heads, n_pages, sinks, recent, to,
@@ -246,7 +255,8 @@ class KvCache:
         return out
 
     def attention_workspace(self, step: Step, heads: int, max_new: Optional[int] = None, n_select: int = 0) -> torch.Tensor:
-        args = _Attention(heads=heads, max_new=step.max_tokens if max_new is None else max_new, n_select=n_select)
+        max_new = step.max_tokens if max_new is None else _int32(max_new, "max_new")
+        args = _Attention(heads=heads, max_new=max_new, n_select=_int32(n_select, "n_select"))
         return self._workspace(_lib().ivfpq_kv_attention_workspace_bytes(self._ref, self._step(step), ctypes.byref(args)))
 
     def attention(self, q: torch.Tensor, step: Step, scale: Optional[float] = None, window: int = 0,
@@ -271,8 +281,8 @@ class KvCache:
             lists = _ptr(pages, torch.int32, (T, self.kv_heads, n_select), dev, "pages") or None
             if n_select < 1:
                 raise ValueError("pages: at least one page for a token and kv head")
-        if max_new is None:
-            max_new = max(T, 1)
+        max_new = max(T, 1) if max_new is None else _int32(max_new, "max_new")
+        window = _int32(window, "window")
         ws = self.attention_workspace(step, heads, max_new, n_select) if workspace is None else workspace
         size = ws.shape[0]
         args = _Attention(qr, heads, max_new, self.head_dim ** -0.5 if scale is None else scale, window, lists, n_select,

@@ -101,3 +101,20 @@ def test_every_call_makes_its_device_the_current_one(kv, monkeypatch):
     s.cache.select(q, s.step, 2)
     s.cache.attention(q, s.step)
     assert entered == [0] * 4
+
+
+def test_numbers_beyond_32_bits_are_refused(kv):
+    """Not cut to what is left of them: a window of 2^32 + 1 is not one of 1."""
+    s = Server(kv, np.random.default_rng(4), "bf16", 2, 64, 6, 2, 3)
+    s.fill([5, 3])
+    q, _ = rows(s.rng, "bf16", 8, 4, 64)
+    big = (1 << 32) + 1
+    for call in (lambda: s.cache.attention(q, s.step, window=big), lambda: s.cache.attention(q, s.step, window=-big),
+                 lambda: s.cache.attention(q, s.step, max_new=big), lambda: s.cache.attention_workspace(s.step, 4, max_new=big),
+                 lambda: s.cache.attention_workspace(s.step, 4, n_select=big), lambda: s.cache.select(q, s.step, big),
+                 lambda: s.cache.select(q, s.step, 2, sinks=big), lambda: s.cache.select(q, s.step, 2, recent=big),
+                 lambda: kv.KvCache(1, big, 64), lambda: kv.KvCache(1, 1, big + 63)):
+        with pytest.raises(ValueError):
+            call()
+    s.attend(4, window=(1 << 31) - 1)
+    s.attend(4, max_new=(1 << 31) - 1)
