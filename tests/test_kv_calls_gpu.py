@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import kv_reference as ref
-from test_kv_gpu import Server, compare, dev, kv, rows  # noqa: F401
+from test_kv_gpu import TYPES, Server, compare, dev, kv, rows  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -118,3 +118,29 @@ def test_numbers_beyond_32_bits_are_refused(kv):
             call()
     s.attend(4, window=(1 << 31) - 1)
     s.attend(4, max_new=(1 << 31) - 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("H,D", [(1, 64), (3, 96), (2, 128), (2, 256)])
+def test_append_writes_the_same_bytes_in_any_pieces(kv, dtype, H, D):
+    """Prompts of every remainder, single tokens, a few at a time, against the same tokens in one call: pages and boxes bit for
+    bit, tokens that are not finite among them, rounded rows too."""
+    rng = np.random.default_rng(D + H)
+    steps = [[0, 1, 63, 64, 65, 130], [1] * 6, [1] * 6, [3, 0, 2, 5, 1, 66], [1] * 6, [7, 70, 4, 1, 128, 2], [2] * 6]
+    s = Server(kv, rng, dtype, H, D, 40, 6, 8)
+    kept = []
+    for new in steps:
+        T = s.plan(new)
+        k, v = (rows(rng, dtype, T, H, D)[0] for _ in range(2))
+        k[T // 2, 0, 5] = float("nan")
+        to = torch.zeros_like(k), torch.zeros_like(v)
+        s.cache.append(k, v, s.step.slots, rounded=to)
+        kept.append((k, v, *to, s.step.slots, s.step.requests, s.step.positions))
+    k, v, kr, vr, slots, request, position = (torch.cat(x) for x in zip(*kept))
+    order = torch.argsort(request.long() * 10000 + position)
+    once = kv.KvCache(40, H, D, TYPES[dtype])
+    to = torch.zeros_like(k), torch.zeros_like(v)
+    once.append(k[order], v[order], slots[order], rounded=to)
+    assert torch.equal(once.pages, s.cache.pages) and torch.equal(once.boxes, s.cache.boxes)
+    assert torch.equal(to[0].view(torch.int16), kr[order].view(torch.int16)) and torch.equal(to[1].view(torch.int16), vr[order].view(torch.int16))
+    assert int((once.pages != 0).sum()) > 0 and to[0].isnan().any()
