@@ -122,10 +122,12 @@ _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cud
 def _launch(device: int, call, *args) -> None:
     """`call` with the stream that is current on the tensors' device, which is made the current one: the library launches there."""
     if _current_device() == device:
-        _check(call(*args, _raw_stream(device)))
+        status = call(*args, _raw_stream(device))
     else:
         with torch.cuda.device(device):
-            _check(call(*args, _raw_stream(device)))
+            status = call(*args, _raw_stream(device))
+    if status:
+        _check(status)
 
 
 class Step:
@@ -264,8 +266,10 @@ class KvCache:
                   lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
         """The new tokens' attention over the cache (`ivfpq_kv_attention`), the new tokens among the keys.
         q [T][heads][head_dim]; scale: head_dim ** -0.5 unless given; window: tokens seen, the token itself among
-        them (0: all); pages: [T][kv_heads][n] int32 from `select`; max_new: no request has more new tokens (a hint
-        that decides how the work is cut; T unless given).  Returns (out as q, lse [T][heads] fp32)."""
+        them (0: all); pages: [T][kv_heads][n] int32 as from `select`, in any order, none twice (its tokens would count
+        twice); max_new: no request has more new tokens (T unless given).  It decides how the work is cut and not what is
+        computed: without it a batch that decodes goes through the kernel of chunks, which takes longer.  Returns
+        (out as q, rows that do not overlap; lse [T][heads] fp32)."""
         T, heads, dev, dtype = step.max_tokens, _heads_of(q), self.device, self.dtype
         shape = (T, heads, self.head_dim)
         qr = _rows(q, dtype, shape, dev, "q")
@@ -281,8 +285,10 @@ class KvCache:
             lists = _ptr(pages, torch.int32, (T, self.kv_heads, n_select), dev, "pages") or None
             if n_select < 1:
                 raise ValueError("pages: at least one page for a token and kv head")
-        max_new = max(T, 1) if max_new is None else _int32(max_new, "max_new")
-        window = _int32(window, "window")
+        if max_new is None:
+            max_new = max(T, 1)
+        if not (0 <= window < 1 << 31 and 0 < max_new < 1 << 31):
+            _int32(window, "window"), _int32(max_new, "max_new")
         ws = self.attention_workspace(step, heads, max_new, n_select) if workspace is None else workspace
         size = ws.shape[0]
         args = _Attention(qr, heads, max_new, self.head_dim ** -0.5 if scale is None else scale, window, lists, n_select,
