@@ -1,14 +1,14 @@
 /*
- * ivfpq_kv.h -- C ABI of the paged 4-bit key/value cache: the search path's idea, cheap bounds
- * that rule lists out and short codes that are read exactly, for the vectors that a decoder
+ * ivfpq_kv.h -- C ABI of the paged 4-bit key/value cache: the search path's idea, boxes
+ * that say where to look and short codes that are read exactly, for the vectors that a decoder
  * looks up at every token.
  *
  * A step of a server runs
  *   1. ivfpq_kv_plan       page tables and slot maps, on the GPU, from the requests' lengths;
  *   2. ivfpq_kv_append     keys and values of the new tokens, rounded to 4 bits, into the pages,
  *                          with a box (per channel minimum and maximum of the keys) per page;
- *   3. ivfpq_kv_select     optional: for every new token and kv head the pages whose boxes
- *                          promise the largest inner products;
+ *   3. ivfpq_kv_select     optional: for every new token and kv head the pages with the largest
+ *                          inner products, as their boxes let one expect;
  *   4. ivfpq_kv_attention  the new tokens' attention over all pages or over the selected ones.
  *
  * Conventions are those of ivfpq.h: device pointers on the current device, nothing is retained,
@@ -137,8 +137,9 @@ int ivfpq_kv_select(const ivfpq_kv_cache *cache, const ivfpq_kv_step *step, ivfp
 typedef struct {
   ivfpq_kv_rows q;
   int32_t heads;           /* a multiple of kv_heads                                          */
-  int32_t max_new;         /* no request has more new tokens; chooses the kernel, 1 for decode */
-  float scale;             /* finite                                                          */
+  int32_t max_new;         /* no request has more new tokens; only chooses the kernel: give 1 for decode, whose kernel
+                              is another than that of chunks                                  */
+  float scale;             /* finite; sizes below 2^-126 count as 2^-126                      */
   int32_t window;          /* 0: none                                                         */
   const int32_t *selected; /* device [max_tokens][kv_heads][n_select], or NULL                */
   int32_t n_select;

@@ -2,9 +2,9 @@
 //
 // The running form of the softmax: with s_j = scale log2(e) q . k_j, a row keeps m = max s_j (or a number near it),
 // l = sum 2^(s_j - m) and o = sum 2^(s_j - m) v_j and multiplies l and o by 2^(m_old - m_new) when m
-// grows; parts of the keys joined the same way.  Sums and statistics are in 32 bits, weights are
-// rounded to the cache's type for the second product (as the values are: both factors exact or
-// within half a unit of the result's type).
+// grows; parts of the keys joined the same way.  Sums and statistics are in 32 bits.  Weights are
+// rounded to the cache's type for the second product, whose other factor, a held value, is exact in it: half a unit of the
+// result's type at most, as rounding the result, and the products run at the 16-bit rate.
 //
 // Layout.  A wavefront works on S^T = K Q^T and O^T = V^T P^T, 16 rows (query heads of one kv head, tokens above
 // them) at a time, so that a lane holds one row's statistics and the exponentials of the first
@@ -946,15 +946,19 @@ Shape shape_of(int64_t tokens, int64_t requests, int kv_heads, int group, int D,
     if (seen < most) most = seen;
   }
   // 16 rows a tile up to 64 rows of a request and head (16 requests of 8001 tokens, 64 rows: 91 us, in a tile of the
-  // chunks' kernel 95; 64 rows of one of 32 000: 35 and 51; 128 rows go either way: 168 and 108, 49 and 56).
+  // chunks' kernel 95; 64 rows of one of 32 000: 35 and 51; 128 rows go either way: 168 and 108, 49 and 56).  Both are
+  // three to five times what reading the pages once takes (28 and 7 us): a page is unpacked for every tile.
   const bool few = n_select > 0 || rows <= 64;
   // Whole units where they are short: 32 requests of 1900 tokens 19 us, in shares and joined 24, 4 requests 15 and 13, one of
-  // 334 7.7 and 11; up to twice as long where there are enough of them: 32 requests of 3900 30 us and 36, 4 requests 24 and 16.
+  // 334 7.7 and 11; up to twice as long where there are enough of them: 32 requests of 3900 30 us and 36, 4 requests 24 and 16.  Just beyond,
+  // requests of one length still gain (32 of 5000: 34 and 39, 64 of 8000: 103 and 107) or not (16 of 5000: 32 and 28); shares
+  // have them, as ragged ones leave whole units waiting for the longest.
   const bool narrow = most <= WHOLE_PAGES || (few && most <= 2 * WHOLE_PAGES && tokens * kv_heads >= 128);
   // Chunks: tiles of 256 rows where they fill the CUs (a page is unpacked by twice the wavefronts: 2048 tokens,
   // 32 heads, behind 8190: 331 us, 128 rows 379; 4 x 700 behind 2000: 162 and 172), of 128 otherwise, and of 64 where units
   // are short, so that shares cannot fill the chip instead (1700 tokens, 16 heads of their own keys, a window of 1000:
-  // 38 us, 128 rows 44).  256 channels have no registers for more than 16 rows a wavefront.
+  // 38 us, 128 rows 44; 3 x 300, 8 heads: 32 and 44; 4 x 200, 8 heads of two, no window: 23 and 30; 2 x 400, 8 heads of four,
+  // a window of 1500: 47 and 48).  256 channels have no registers for more than 16 rows a wavefront.
   const int64_t all = tokens * group * kv_heads;
   s.tile_rows = few ? 16 : D == 256 ? 128 : all >= 256 * 256 ? 256 : narrow && all < 512 * 128 ? 64 : 128;
   const int64_t units = n_select > 0 ? tokens * kv_heads * ((group + 15) / 16)

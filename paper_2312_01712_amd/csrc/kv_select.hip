@@ -1,11 +1,14 @@
-// Pages for every new token and kv head, by an upper bound on the inner products with the keys of a
+// Pages for every new token and kv head, by an estimate of the largest inner product with the keys of a
 // page: the box of the keys takes the place of the per-list boxes of the search path.
 //
 //   score(page) = max over the query heads of sum_d max(q_d lo_d, q_d hi_d) * 2^e
 //               = max over the query heads of (min(q, 0) . lo + max(q, 0) . hi) * 2^e
 //
 // a product of length 2 D with the box as it lies in memory, [lo | hi].  Queries and corners are 8-bit
-// whole numbers, so the products run on the int8 matrix units and the sums are exact in any order.
+// whole numbers, so the products run on the int8 matrix units and the sums are exact in any order.  Corners are rounded
+// outwards, queries to the nearest, so that the score can be below the box's own bound (of normal keys and queries it is in a
+// third of the pages); it ranks pages and rules none out.  Of 48 of 1000 pages and 128 of 4000, 99 % are those of the
+// unrounded scores.
 //
 // kv_score_kernel: bound by the boxes, 4 D bytes a page and head; a wavefront has 16 pages, a lane
 // 16 channels of one page per step of 64, rounds them to bytes itself (the boxes stay in bf16, where
