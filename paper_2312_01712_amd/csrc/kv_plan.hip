@@ -11,7 +11,7 @@
 // pages ran out its row has -1, and those in the ring would let it claim more pages than there are.
 // So its row is counted before anything is placed: with few requests by every workgroup, for the requests up to its own;
 // otherwise by a launch of its own, which leaves sums of 16 requests too, so that no workgroup reads all lengths.
-// Bound by the launch and a few dependent trips to L2: 4.1 us for one request of 37 tokens, 3.5 and 9.0 us for 4001 requests
+// Bound by the launch and a few dependent trips to L2: 4.2 us for one request of 37 tokens, 3.8 and 9.1 us for 4001 requests
 // (15 000 new tokens, 250 of them ended with up to 2046 pages each).
 
 #include "kv_internal.h"
