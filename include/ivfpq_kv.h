@@ -11,6 +11,13 @@
  *                          inner products, as their boxes let one expect;
  *   4. ivfpq_kv_attention  the new tokens' attention over all pages or over the selected ones.
  *
+ * A step that checks drafted tokens, a tree of them a request, runs
+ *   1. ivfpq_kv_plan            as above, every drafted token a new one;
+ *   2. ivfpq_kv_tree_plan       what each of them sees of the others, and its position;
+ *   3. ivfpq_kv_rotate          queries and keys turned by those positions (or by any others);
+ *   4. ivfpq_kv_append, ivfpq_kv_tree_attention   in each layer;
+ *   5. ivfpq_kv_keep            what stays of them, in the caches of all layers.
+ *
  * Conventions are those of ivfpq.h: device pointers on the current device, nothing is retained,
  * nothing is allocated, nothing synchronises; kernels go to `hip_stream`; return values are
  * ivfpq_status and ivfpq_last_error() has the text; on an argument error nothing is enqueued.
@@ -49,7 +56,7 @@ extern "C" {
 typedef enum { IVFPQ_KV_BF16 = 0, IVFPQ_KV_FP16 = 1 } ivfpq_kv_dtype;
 
 /* The caller's memory that holds a cache.  `pages` is filled with zeros once, before its first
- * use, and from then on written by ivfpq_kv_append only. */
+ * use, and from then on written by ivfpq_kv_append and ivfpq_kv_keep only (or filled with what such a cache held). */
 typedef struct {
   int64_t n_pages;  /* 1 .. 2^25                                                     */
   int32_t kv_heads; /* 1 .. 1024                                                     */
@@ -154,6 +161,80 @@ size_t ivfpq_kv_attention_workspace_bytes(const ivfpq_kv_cache *cache, const ivf
                                           const ivfpq_kv_attention_args *args);
 int ivfpq_kv_attention(const ivfpq_kv_cache *cache, const ivfpq_kv_step *step, const ivfpq_kv_attention_args *args,
                        void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Rows that are written: as ivfpq_kv_rows; they must not overlap each other. */
+typedef struct {
+  void *data;
+  int64_t token_stride, head_stride;
+} ivfpq_kv_out_rows;
+
+/* Rotary positions.  Pair i of a row's first `turned` channels, channels i and i + turned / 2 or (neighbours) 2 i and 2 i + 1, is
+ * turned by the angle positions[axis[i]] * f_i:  (a, b) -> (a cos - b sin, b cos + a sin).  Frequencies are given in turns, as 64-bit
+ * fractions of one: phases[i] = round(f_i / (2 pi) * 2^64) modulo 2^64, so that far positions lose nothing. */
+#define IVFPQ_KV_MAX_AXES 8
+typedef struct {
+  int32_t head_dim;       /* 64, 96, 128 or 256                                                  */
+  int32_t turned;         /* a multiple of 16, head_dim at most; the other channels stay as they are */
+  int32_t neighbours;
+  int32_t dtype;          /* an ivfpq_kv_dtype                                                   */
+  int32_t axes;           /* 1 .. IVFPQ_KV_MAX_AXES                                              */
+  const uint64_t *phases; /* device [turned / 2]                                                 */
+  const int32_t *axis;    /* device [turned / 2], each below axes (others count as 0)            */
+} ivfpq_kv_rotary;
+
+/* positions: device [axes][tokens] int32, axis_stride between two axes.  A token whose position on axis 0 is negative is no token:
+ * its rows are neither read nor written; on other axes any position may be negative.  The rows written may be the rows read
+ * (same address and strides); otherwise they must not overlap them, nor q_out k_out.  heads or kv_heads may be 0. */
+int ivfpq_kv_rotate(const ivfpq_kv_rotary *rotary, ivfpq_kv_rows q, int32_t heads, ivfpq_kv_rows k, int32_t kv_heads,
+                    const int32_t *positions, int64_t axis_stride, int64_t tokens, ivfpq_kv_out_rows q_out, ivfpq_kv_out_rows k_out,
+                    void *hip_stream);
+
+/* Trees of drafted tokens.  Token i of a request (its i-th new one in the step) has a parent, an earlier token of the
+ * request's new ones, or none; it sees itself, its parent, that one's parent and so on. */
+#define IVFPQ_KV_MAX_NODES 1024
+typedef struct {
+  int32_t max_nodes;   /* no request has more new tokens, 1 .. IVFPQ_KV_MAX_NODES; tokens beyond it see none of the new ones */
+  int32_t window;      /* 0: none; otherwise a token sees itself and the window - 1 positions before it */
+  uint64_t *masks;     /* device [max_tokens][(max_nodes + 63) / 64]: bit j % 64 of word j / 64: token j is seen */
+  int32_t *positions;  /* device [max_tokens]: position of the request's first new token, plus the ancestors' number; -1: no token */
+} ivfpq_kv_tree;
+
+/* Fills masks and positions.  parents: device [max_tokens], the parent's number within its request; whatever is no earlier token
+ * of the request (-1) is none.  step: as ivfpq_kv_plan has left it. */
+int ivfpq_kv_tree_plan(const ivfpq_kv_step *step, const int32_t *parents, const ivfpq_kv_tree *tree, void *hip_stream);
+
+/* The drafted tokens' attention: as ivfpq_kv_attention, but a token sees the positions below that of its request's first new
+ * token, and of the new ones those that its mask names (any mask may be given; bits of tokens that are not there are not looked at).
+ * With a window of the tree it sees of the former those above positions[t] - window, where positions[t] is taken between those of the
+ * request's first and last new token; masks are taken as they are.  selected, n_select must be NULL and 0; max_new and window of `args`
+ * are not looked at. */
+size_t ivfpq_kv_tree_attention_workspace_bytes(const ivfpq_kv_cache *cache, const ivfpq_kv_step *step,
+                                               const ivfpq_kv_attention_args *args, const ivfpq_kv_tree *tree);
+int ivfpq_kv_tree_attention(const ivfpq_kv_cache *cache, const ivfpq_kv_step *step, const ivfpq_kv_attention_args *args,
+                            const ivfpq_kv_tree *tree, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* What stays of a step's drafted tokens.  A request's first new token agrees; another that is stored agrees if drafted[it] ==
+ * picked[its parent] (its parent: the last token before it that its mask names).  The deepest token whose mask names only tokens that
+ * agree, the first among equals, and what it sees stay, in this order, behind what was held; the request's other new tokens are
+ * held no more.  tree: one without a window.
+ *   drafted, picked  device [max_tokens] int32: the tokens, and those that the model picks behind each
+ *   lens    device [requests]: tokens held from now on, past_lens of the next step
+ *   rows    device [max_tokens]: from q_start[r] on the rows that stay of request r, -1 behind them
+ *   counts  device [requests]: room in which the pages that go back are counted
+ * In every cache the bytes of what stays move to the slots behind what was held, the boxes of their pages become those of
+ * the keys that these hold then (bit for bit what appending only these tokens gives), and pages behind what stays are put into the
+ * ring, in the order of requests and positions, as ivfpq_kv_plan puts those of ended requests: free_state is what the plan of the
+ * step has left, free_state_out what the next plan starts from.  The table's entries stay as they are.  A token that is not
+ * stored (a page was missing) does not stay, unless it is the request's first.  Once per step: done again, the moved
+ * tokens would move again.  caches: 1 to 1024 of one shape and type that share the step. */
+int ivfpq_kv_keep(const ivfpq_kv_cache *caches, int32_t n_caches, const ivfpq_kv_step *step, const ivfpq_kv_tree *tree,
+                  const int32_t *drafted, const int32_t *picked, int32_t *free_pages, int64_t free_capacity, const int64_t *free_state,
+                  int64_t *free_state_out, int32_t *lens, int32_t *rows, int32_t *counts, void *hip_stream);
+
+/* Held keys and values at `slots` (device int64) as rows of the cache's type, exactly as they are held; keys of a token
+ * that is no number are NaN, rows of slots outside the cache 0. */
+int ivfpq_kv_read(const ivfpq_kv_cache *cache, const int64_t *slots, int64_t tokens, ivfpq_kv_out_rows k, ivfpq_kv_out_rows v,
+                  void *hip_stream);
 
 #ifdef __cplusplus
 }

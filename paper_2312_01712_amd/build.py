@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libivfpq_hip.so")
 SOURCES = ["api.hip", "coarse.hip", "scan.hip", "scan_rt.hip", "scan_lm.hip", "radius.hip",
-           "kv_api.hip", "kv_plan.hip", "kv_append.hip", "kv_select.hip", "kv_attention.hip"]
+           "kv_api.hip", "kv_plan.hip", "kv_append.hip", "kv_select.hip", "kv_attention.hip",
+           "kv_tree_api.hip", "kv_rotate.hip", "kv_tree.hip", "kv_tree_attention.hip", "kv_keep.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -61,6 +61,9 @@ struct KvAttnArgs {
   const int32_t *table, *q_start, *kv_lens, *token_req, *positions, *selected;
   int64_t q_token, q_head, out_token, out_head, n_pages;
   int32_t kv_heads, group, requests, tokens, width, n_select, window;
+  const uint64_t *masks;          // trees: [tokens][words]
+  const int32_t *tree_positions;  // [tokens]
+  int32_t words;
   float scale2;  // |scale| log2(e), above 0
   int32_t negative;  // the scale was below 0
   // workgroups; whether each has a whole unit of rows instead of a share of all units' pages; whether prefix is filled
@@ -70,6 +73,54 @@ struct KvAttnArgs {
   float *part_ml;    // [2 n_wg][rows of a tile][2]: parts of units that go across borders
   float *part_o;     // [2 n_wg][rows of a tile][D]
 };
+
+struct KvRotateArgs {
+  const uint16_t *q, *k;
+  uint16_t *q_out, *k_out;
+  const int32_t *positions, *axis;
+  const uint64_t *phases;
+  int64_t q_token, q_head, k_token, k_head, qo_token, qo_head, ko_token, ko_head, axis_stride, tokens;
+  int32_t heads, kv_heads, axes, turned, dim, per, slots;  // per: heads of a thread; slots: threads that share a token's heads
+};
+
+struct KvTreeArgs {
+  const int32_t *q_start, *positions, *parents;
+  uint64_t *masks;
+  int32_t *tree_positions;
+  int32_t requests, tokens, max_nodes, words, window;
+};
+
+constexpr int KEEP_CACHES = 64;  // of one launch
+
+struct KvKeepArgs {
+  const int32_t *q_start, *kv_lens, *positions, *drafted, *picked;
+  const int32_t *table;
+  const int64_t *slots, *state;
+  const uint64_t *masks;
+  int32_t *lens, *rows, *counts, *free_pages;
+  int64_t *state_out;
+  int64_t n_pages, capacity;
+  int32_t requests, tokens, width, max_nodes, words, kv_heads, n_caches;
+  char *pages[KEEP_CACHES];
+  uint16_t *boxes[KEEP_CACHES];
+};
+
+struct KvReadArgs {
+  const char *pages;
+  const int64_t *slots;
+  uint16_t *k, *v;
+  int64_t k_token, k_head, v_token, v_head, n_slots, tokens;
+  int32_t kv_heads;
+};
+
+int launch_kv_rotate(const KvRotateArgs &a, int neighbours, int dtype, hipStream_t s);
+int launch_kv_tree(const KvTreeArgs &a, hipStream_t s);
+int launch_kv_accept(const KvKeepArgs &a, hipStream_t s);
+int launch_kv_move(const KvKeepArgs &a, int D, int dtype, bool ring, hipStream_t s);
+int launch_kv_read(const KvReadArgs &a, int D, int dtype, hipStream_t s);
+size_t kv_tree_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_nodes, int window,
+                                   int64_t width);
+int launch_kv_tree_attention(const KvAttnArgs &a, int D, int dtype, int max_nodes, char *workspace, hipStream_t s);
 
 int launch_kv_plan(const KvPlanArgs &a, hipStream_t s);
 int launch_kv_append(const KvAppendArgs &a, int D, int dtype, hipStream_t s);

@@ -9,24 +9,36 @@ One step of a server that decodes `requests` requests:
     pages = cache.select(q, step, 64)                           # optional: 64 pages a token and kv head
     out, lse = cache.attention(q, step, pages=pages, max_new=1)     # q [T][heads][head_dim]
     past_lens, free_state = step.kv_lens, step.free_state
+
+One that checks drafted tokens, a tree of them a request (its first token is the last one that is certain):
+
+    step = kv.plan(past_lens, new_lens, table, free_pages, free_state, max_tokens=T)
+    tree = kv.tree(parents, step, max_nodes=N)                  # what each sees of the others, and its position
+    q, k = rotary(q, k, tree.positions)                         # rotary = kv.Rotary(frequencies, axes), once
+    cache.append(k, v, step.slots)
+    out, lse = cache.tree_attention(q, step, tree)              # these three in each layer
+    kept = kv.keep(caches, step, tree, drafted, picked, free_pages, step.free_state)   # all layers' caches
+    past_lens, free_state = kept.lens, kept.free_state
 """
 from __future__ import annotations
 
 import ctypes
-from typing import Optional, Tuple
+from fractions import Fraction
+from typing import Optional, Sequence, Tuple
 
 import torch
 
 from .binding import IvfpqError, _check, _dev, load_library  # noqa: F401
 
 PAGE = 64
-MAX_REQUESTS, MAX_SELECT = 65536, 1024
+MAX_REQUESTS, MAX_SELECT, MAX_NODES, MAX_AXES = 65536, 1024, 1024, 8
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 # every symbol include/ivfpq_kv.h declares
 SYMBOLS = [
     "ivfpq_kv_page_bytes", "ivfpq_kv_plan", "ivfpq_kv_append", "ivfpq_kv_select_workspace_bytes", "ivfpq_kv_select",
-    "ivfpq_kv_attention_workspace_bytes", "ivfpq_kv_attention",
+    "ivfpq_kv_attention_workspace_bytes", "ivfpq_kv_attention", "ivfpq_kv_rotate", "ivfpq_kv_tree_plan",
+    "ivfpq_kv_tree_attention_workspace_bytes", "ivfpq_kv_tree_attention", "ivfpq_kv_keep", "ivfpq_kv_read",
 ]
 
 _vp, _i64, _i32, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
@@ -51,6 +63,15 @@ class _Attention(ctypes.Structure):
                 ("lse", _vp)]
 
 
+class _Rotary(ctypes.Structure):
+    _fields_ = [("head_dim", _i32), ("turned", _i32), ("neighbours", _i32), ("dtype", _i32), ("axes", _i32), ("phases", _vp),
+                ("axis", _vp)]
+
+
+class _Tree(ctypes.Structure):
+    _fields_ = [("max_nodes", _i32), ("window", _i32), ("masks", _vp), ("positions", _vp)]
+
+
 _ready = None
 
 
@@ -69,6 +90,14 @@ def _lib():
         lib.ivfpq_kv_attention_workspace_bytes.argtypes = [cp, sp, ap]
         lib.ivfpq_kv_attention_workspace_bytes.restype = _sz
         lib.ivfpq_kv_attention.argtypes = [cp, sp, ap, _vp, _sz, _vp]
+        tp = ctypes.POINTER(_Tree)
+        lib.ivfpq_kv_rotate.argtypes = [ctypes.POINTER(_Rotary), _Rows, _i32, _Rows, _i32, _vp, _i64, _i64, _Rows, _Rows, _vp]
+        lib.ivfpq_kv_tree_plan.argtypes = [sp, _vp, tp, _vp]
+        lib.ivfpq_kv_tree_attention_workspace_bytes.argtypes = [cp, sp, ap, tp]
+        lib.ivfpq_kv_tree_attention_workspace_bytes.restype = _sz
+        lib.ivfpq_kv_tree_attention.argtypes = [cp, sp, ap, tp, _vp, _sz, _vp]
+        lib.ivfpq_kv_keep.argtypes = [_vp, _i32, sp, tp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp]
+        lib.ivfpq_kv_read.argtypes = [cp, _vp, _i64, _Rows, _Rows, _vp]
         _ready = lib
     return _ready
 
@@ -188,6 +217,141 @@ def plan(past_lens: torch.Tensor, new_lens: torch.Tensor, table: torch.Tensor, f
     return out
 
 
+class Tree:
+    """What `tree` leaves for attention and `keep`: masks [T][ceil(max_nodes / 64)] int64 (bit j % 64 of word j / 64: the request's
+    j-th new token is seen), positions [T] int32 (-1 in rows without a token)."""
+
+    def __init__(self, masks: torch.Tensor, positions: torch.Tensor, max_nodes: int, window: int = 0):
+        if not 1 <= max_nodes <= MAX_NODES:
+            raise ValueError(f"max_nodes = {max_nodes} outside [1, {MAX_NODES}]")
+        if not 0 <= window < 1 << 31:
+            raise ValueError(f"window = {window} outside [0, 2^31)")
+        T = masks.shape[0]
+        self._checked = dev = _dev(masks, torch.int64, (T, (max_nodes + 63) // 64), what="masks").device.index
+        _dev(positions, torch.int32, (T,), dev, "positions")
+        self.masks, self.positions, self.max_nodes, self.window, self.max_tokens = masks, positions, max_nodes, window, T
+        self._c = _Tree(max_nodes, window, masks.data_ptr(), positions.data_ptr())
+        self._ref, self._held = ctypes.byref(self._c), (masks, positions)
+
+    @classmethod
+    def empty(cls, max_tokens: int, max_nodes: int, window: int = 0, device=None) -> "Tree":
+        """Buffers for the trees of a step, to be filled by `tree(..., out=tree)`."""
+        device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        return cls(torch.empty(max_tokens, (max_nodes + 63) // 64, dtype=torch.int64, device=device),
+                   torch.empty(max_tokens, dtype=torch.int32, device=device), max_nodes, window)
+
+
+def _fits(step: Step, tree: Tree) -> None:
+    if tree.max_tokens != step.max_tokens or tree._checked != step._checked:
+        raise ValueError(f"tree: {tree.max_tokens} rows on cuda:{tree._checked}, the step has {step.max_tokens} on cuda:{step._checked}")
+
+
+def tree(parents: torch.Tensor, step: Step, max_nodes: Optional[int] = None, window: int = 0, out: Optional[Tree] = None) -> Tree:
+    """What drafted tokens see of each other, and their positions (`ivfpq_kv_tree_plan`).  parents [T] int32: the number, within
+    its request, of the token that each hangs on; -1: none.  max_nodes: no request has more new tokens (T unless given, 1024 at
+    most); window: positions that a token sees, its own among them (0: all)."""
+    if out is None:
+        out = Tree.empty(step.max_tokens, min(max(step.max_tokens, 1), MAX_NODES) if max_nodes is None else max_nodes, window,
+                         step.table.device)
+    elif (max_nodes is not None and max_nodes != out.max_nodes) or (window and window != out.window):
+        raise ValueError(f"tree: out was made for max_nodes = {out.max_nodes} and window = {out.window}")
+    _fits(step, out)
+    dev = step._checked
+    _launch(dev, _lib().ivfpq_kv_tree_plan, step._ref, _ptr(parents, torch.int32, (step.max_tokens,), dev, "parents"), out._ref)
+    return out
+
+
+# 2 pi 2^200, rounded: frequencies are divided by it as whole numbers
+_TWO_PI = 10096689509235987743946820282484873672429286842977325943070736
+
+
+class Rotary:
+    """Rotary positions (`ivfpq_kv_rotate`).  frequencies: radians a position, one for each pair of channels (their number a
+    multiple of 8: the first 2 len(frequencies) channels are turned); axes: which axis of the position turns each pair (all the first,
+    unless given), such as time, height and width; neighbours: pairs are channels 2 i and 2 i + 1 instead of i and i + len(frequencies)."""
+
+    def __init__(self, frequencies: Sequence[float], axes: Optional[Sequence[int]] = None, neighbours: bool = False, device=None):
+        frequencies = [float(f) for f in frequencies]
+        axes = [0] * len(frequencies) if axes is None else [int(a) for a in axes]
+        if not frequencies or len(frequencies) % 8 or len(frequencies) > 128:
+            raise ValueError(f"{len(frequencies)} frequencies: a multiple of 8 up to 128 is needed")
+        if len(axes) != len(frequencies) or not all(0 <= a < MAX_AXES for a in axes):
+            raise ValueError(f"axes: one of 0 .. {MAX_AXES - 1} is needed for each of the {len(frequencies)} frequencies")
+        if not all(abs(f) < float("inf") for f in frequencies):
+            raise ValueError("frequencies must be finite")
+        turns = [round(Fraction(f) * (1 << 264) / _TWO_PI) % (1 << 64) for f in frequencies]
+        device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        self._phases = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device=device)
+        self._axis = torch.tensor(axes, dtype=torch.int32, device=device)
+        self.device, self.axes, self.turned, self.neighbours = self._phases.device.index, max(axes) + 1, 2 * len(turns), bool(neighbours)
+
+    def __call__(self, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
+                 out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """q [T][heads][head_dim] and k [T][kv_heads][head_dim] turned by positions [axes][T] int32 ([T]: the same on every axis);
+        a token whose first position is negative is left out: its rows are not written.  out: two tensors for the results, q and k
+        themselves among them; no other overlap."""
+        heads, kv_heads, dev = _heads_of(q), _heads_of(k), self.device
+        T, _, D = q.shape
+        if q.dtype not in _DTYPES:
+            raise ValueError(f"q must be of torch.bfloat16 or torch.float16, not {q.dtype}")
+        dtype = q.dtype
+        qr, kr = _rows(q, dtype, (T, heads, D), dev, "q"), _rows(k, dtype, (T, kv_heads, D), dev, "k")
+        one = isinstance(positions, torch.Tensor) and positions.dim() == 1
+        at = _ptr(positions, torch.int32, (T,) if one else (self.axes, T), dev, "positions")
+        if out is None:
+            out = torch.empty((T, heads, D), dtype=dtype, device=q.device), torch.empty((T, kv_heads, D), dtype=dtype, device=q.device)
+        to_q, to_k = _rows(out[0], dtype, (T, heads, D), dev, "out q"), _rows(out[1], dtype, (T, kv_heads, D), dev, "out k")
+        c = _Rotary(D, self.turned, self.neighbours, _DTYPES[dtype], self.axes, self._phases.data_ptr(), self._axis.data_ptr())
+        _launch(dev, _lib().ivfpq_kv_rotate, ctypes.byref(c), qr, heads, kr, kv_heads, at, 0 if one else T, T, to_q, to_k)
+        return out[0], out[1]
+
+
+class Kept:
+    """What `keep` leaves: lens [R] int32, the tokens that each request holds from now on; rows [T] int32, of request r from
+    q_start[r] on the rows that stay, -1 behind them; free_state [3] int64 of the next plan."""
+
+    def __init__(self, lens: torch.Tensor, rows: torch.Tensor, free_state: torch.Tensor):
+        R, T = lens.shape[0], rows.shape[0]
+        self._checked = dev = _dev(free_state, torch.int64, (3,), what="free_state").device.index
+        _dev(lens, torch.int32, (R,), dev, "lens")
+        _dev(rows, torch.int32, (T,), dev, "rows")
+        self.lens, self.rows, self.free_state = lens, rows, free_state
+        counts = torch.empty(R, dtype=torch.int32, device=lens.device)  # room for keep
+        self._shape = R, T
+        self._at = free_state.data_ptr(), lens.data_ptr(), rows.data_ptr(), counts.data_ptr()
+        self._held = lens, rows, free_state, counts
+
+    @classmethod
+    def empty(cls, step: Step) -> "Kept":
+        """Buffers for `keep(..., out=kept)` after steps of this size."""
+        def new(n, dtype=torch.int32):
+            return torch.empty(n, dtype=dtype, device=step.table.device)
+        return cls(new(step.kv_lens.shape[0]), new(step.max_tokens), new(3, torch.int64))
+
+
+def keep(caches: Sequence["KvCache"], step: Step, tree: Tree, drafted: torch.Tensor, picked: torch.Tensor, free_pages: torch.Tensor,
+         free_state: torch.Tensor, out: Optional[Kept] = None) -> Kept:
+    """What stays of a step's drafted tokens (`ivfpq_kv_keep`): of every request its first new token and the longest path behind
+    it whose tokens are those that the model picked.  They move together in all caches (of one shape), the boxes of their
+    pages are made again, pages behind them go back to the ring.  tree: the step's, without a window; drafted, picked [T] int32: the
+    tokens, and what the model picks behind each; free_state: `step.free_state`.  Once per step."""
+    caches = list(caches)
+    _fits(step, tree)
+    dev, T = step._checked, step.max_tokens
+    if not all(c.device == dev for c in caches):
+        raise ValueError(f"caches: not all on cuda:{dev}, where the step is")
+    if out is None:
+        out = Kept.empty(step)
+    elif out._shape != (step.kv_lens.shape[0], T) or out._checked != dev:
+        raise ValueError(f"keep: out was made for steps of {out._shape} requests and rows on cuda:{out._checked}")
+    state_out, lens, rows, counts = out._at
+    ring = _ptr(free_pages, torch.int32, free_pages.shape[:1], dev, "free_pages")
+    _launch(dev, _lib().ivfpq_kv_keep, (_Cache * len(caches))(*[c._c for c in caches]), len(caches), step._ref, tree._ref,
+            _ptr(drafted, torch.int32, (T,), dev, "drafted"), _ptr(picked, torch.int32, (T,), dev, "picked"), ring, free_pages.shape[0],
+            _ptr(free_state, torch.int64, (3,), dev, "free_state"), state_out, lens, rows, counts)
+    return out
+
+
 class KvCache:
     """Device memory of a paged 4-bit cache: `pages` (uint8, the layout of include/ivfpq_kv.h) and `boxes`
     [n_pages][kv_heads][2][head_dim] bf16, the smallest and largest key value of each channel of a page."""
@@ -296,3 +460,42 @@ class KvCache:
         _launch(dev, _lib().ivfpq_kv_attention, self._ref, self._step(step), ctypes.byref(args),
                 _ptr(ws, torch.uint8, (size,), dev, "workspace"), size)
         return out, lse
+
+    def tree_attention_workspace(self, step: Step, heads: int, tree: Tree) -> torch.Tensor:
+        _fits(step, tree)
+        args = _Attention(heads=heads, max_new=1)
+        return self._workspace(_lib().ivfpq_kv_tree_attention_workspace_bytes(self._ref, self._step(step), ctypes.byref(args), tree._ref))
+
+    def tree_attention(self, q: torch.Tensor, step: Step, tree: Tree, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                       lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+        """Drafted tokens' attention over the cache (`ivfpq_kv_tree_attention`): over what their requests held before the step (with a
+        window of the tree the last of it) and over the new tokens that their masks name.  q [T][heads][head_dim]; scale: head_dim
+        ** -0.5 unless given.  Returns (out as q, rows that do not overlap; lse [T][heads] fp32)."""
+        T, heads, dev, dtype = step.max_tokens, _heads_of(q), self.device, self.dtype
+        _fits(step, tree)
+        shape = (T, heads, self.head_dim)
+        qr = _rows(q, dtype, shape, dev, "q")
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=q.device)
+        to = _rows(out, dtype, shape, dev, "out")
+        if lse is None:
+            lse = torch.empty((T, heads), dtype=torch.float32, device=q.device)
+        to_lse = _ptr(lse, torch.float32, (T, heads), dev, "lse")
+        ws = self.tree_attention_workspace(step, heads, tree) if workspace is None else workspace
+        size = ws.shape[0]
+        args = _Attention(qr, heads, 1, self.head_dim ** -0.5 if scale is None else scale, 0, None, 0, to.data, to.token_stride,
+                          to.head_stride, to_lse)
+        _launch(dev, _lib().ivfpq_kv_tree_attention, self._ref, self._step(step), ctypes.byref(args), tree._ref,
+                _ptr(ws, torch.uint8, (size,), dev, "workspace"), size)
+        return out, lse
+
+    def read(self, slots: torch.Tensor, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Held keys and values at slots [T] int64 as rows [T][kv_heads][head_dim] (`ivfpq_kv_read`); 0 for slots outside the cache."""
+        shape = (slots.shape[0], self.kv_heads, self.head_dim)
+        dtype, dev = self.dtype, self.device
+        at = _ptr(slots, torch.int64, shape[:1], dev, "slots")
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=slots.device), torch.empty(shape, dtype=dtype, device=slots.device)
+        kr, vr = _rows(out[0], dtype, shape, dev, "out k"), _rows(out[1], dtype, shape, dev, "out v")
+        _launch(dev, _lib().ivfpq_kv_read, self._ref, at, shape[0], kr, vr)
+        return out[0], out[1]
