@@ -309,6 +309,7 @@ __global__ __launch_bounds__(1024) void kv_scan_kernel(KvAttnArgs a, int tile_ro
   __shared__ int sums[16];
   const Requests q = {a.prefix, nullptr, nullptr, nullptr};
   const int total = tile_rows == 16 ? scan_units<16, 1024>(a, q, sums, threadIdx.x)
+                      : tile_rows == 32 ? scan_units<32, 1024>(a, q, sums, threadIdx.x)
                       : tile_rows == 64 ? scan_units<64, 1024>(a, q, sums, threadIdx.x)
                       : tile_rows == 128 ? scan_units<128, 1024>(a, q, sums, threadIdx.x)
                                          : scan_units<256, 1024>(a, q, sums, threadIdx.x);
@@ -393,38 +394,24 @@ __device__ inline void leave_border(const KvAttnArgs &a, const Share &s, const U
   b[5] = rows;
 }
 
-// A tree's row: past, the position of the request's first new token, and the words that say which new tokens it sees.
-template <bool TREE>
-struct TreeRow {};
-template <>
-struct TreeRow<true> {
-  int past;
-  const uint64_t *mask;
-  uint64_t first;  // word 0, fetched ahead of the page that needs it
-};
-
 // The row that a lane works on, and which keys the rows of its 16 see: the row itself (low, high]; every row those in
 // (clear_low, clear_high]; none those outside (any_low, any_high].
-template <bool TREE = false>
-struct Place : TreeRow<TREE> {
+struct Place {
   int64_t t;
   int hq, low, high, clear_low, clear_high, any_low, any_high;
 };
 
 template <int TR, bool TREE = false>
-__device__ inline Place<TREE> place_of(const KvAttnArgs &a, const Unit &u, int rows, int in_tile) {
-  Place<TREE> p;
+__device__ inline Place place_of(const KvAttnArgs &a, const Unit &u, int rows, int in_tile) {
+  Place p;
   const int i = u.tile * TR + min(in_tile, rows - 1);
   p.t = u.t0 + i / a.group;
   p.hq = u.head * a.group + i % a.group;
   if constexpr (TREE) {
     // positions do not follow the order of tokens: what is clear is said for all of the request's
-    p.past = min(u.pos0, u.kv);
-    p.mask = a.masks + p.t * a.words;
-    p.first = p.mask[0];
     p.high = u.kv - 1;
     p.low = a.window > 0 ? max(min(max(a.tree_positions[p.t], u.pos0), u.pos0 + u.fresh - 1) - a.window, -1) : -1;
-    p.clear_high = p.past - 1;
+    p.clear_high = min(u.pos0, u.kv) - 1;
     p.any_high = u.kv - 1;
     p.clear_low = a.window > 0 ? max(u.pos0 + u.fresh - 1 - a.window, -1) : -1;
     p.any_low = a.window > 0 ? max(u.pos0 - a.window, -1) : -1;
@@ -442,27 +429,24 @@ __device__ inline Place<TREE> place_of(const KvAttnArgs &a, const Unit &u, int r
   return p;
 }
 
-// Which keys of the page that begins at position `first` a tree's row sees, a bit each: those held before the new tokens, and
-// new ones by the row's mask.
-template <bool TREE>
-__device__ inline uint64_t tree_sees(const KvAttnArgs &a, const Place<TREE> &p, int first) {
+// Which keys of the page that begins at position `first` a tree's token sees, a bit each: those held before the new tokens and above
+// `low`, and new ones by its mask.
+__device__ inline uint64_t tree_sees(const KvAttnArgs &a, const Unit &u, int64_t t, int low, int first) {
+  const int n = min(u.pos0, u.kv) - first;  // keys of the page before the new tokens
   uint64_t x = 0;
-  if constexpr (TREE) {
-    const int n = p.past - first;  // keys of the page before the new tokens
-    if (n < 64) {
-      const int at = max(-n, 0) >> 6, shift = max(-n, 0) & 63;
-      uint64_t word = at == 0 ? p.first : at < a.words ? p.mask[at] : 0;
-      x = n > 0 ? word << n : word >> shift;
-      if (shift != 0 && at + 1 < a.words) x |= p.mask[at + 1] << (64 - shift);
-      const int rest = p.high + 1 - first;  // keys that are held
-      if (rest < 64) x &= rest > 0 ? (1ull << rest) - 1 : 0;
-    }
-    uint64_t held = n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0;
-    const int out = p.low + 1 - first;  // keys that the window leaves out
-    if (out > 0) held &= out < 64 ? ~0ull << out : 0;
-    x |= held;
+  if (n < 64) {
+    const uint64_t *mask = a.masks + t * a.words;
+    const int at = max(-n, 0) >> 6, shift = max(-n, 0) & 63;
+    const uint64_t word = at < a.words ? mask[at] : 0;
+    x = n > 0 ? word << n : word >> shift;
+    if (shift != 0 && at + 1 < a.words) x |= mask[at + 1] << (64 - shift);
+    const int rest = u.kv - first;  // keys that are held
+    if (rest < 64) x &= rest > 0 ? (1ull << rest) - 1 : 0;
   }
-  return x;
+  uint64_t held = n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0;
+  const int out = low + 1 - first;  // keys that the window leaves out
+  if (out > 0) held &= out < 64 ? ~0ull << out : 0;
+  return x | held;
 }
 
 // A lane's part of its row as the second operand of K Q^T: channels g D/4 + 8 c + 0 .. 7.
@@ -483,9 +467,10 @@ __device__ inline float lse_of(float m, float l) {
 }
 
 // A unit's rows from the four wavefronts that had some of its pages each: to the result, or to the workspace.
-template <int D, int DT>
+// tile: which 16 of a unit of NT tiles.
+template <int D, int DT, int NT = 1>
 __device__ inline void join_waves(const KvAttnArgs &a, const Unit &u, int rows, bool whole, int64_t slot, float (*ml)[16][2],
-                                  float *buf, int tid) {
+                                  float *buf, int tid, int tile = 0) {
   // buf [4][16][D + 4], ml [4]
   const int row = tid >> 4, part = tid & 15;
   float m = -__builtin_inff(), l = 0.0f, f[4];
@@ -505,8 +490,8 @@ __device__ inline void join_waves(const KvAttnArgs &a, const Unit &u, int rows, 
     for (int w = 0; w < 4; ++w) x[c] += f[w] * buf[(w * 16 + row) * (D + 4) + part * (D / 16) + c];
   }
   if (whole) {
-    if (row < rows) {
-      const int i = u.tile * 16 + row;
+    if (tile * 16 + row < rows) {
+      const int i = (u.tile * NT + tile) * 16 + row;
       const int64_t t = u.t0 + i / a.group;
       const int hq = u.head * a.group + i % a.group;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -516,12 +501,13 @@ __device__ inline void join_waves(const KvAttnArgs &a, const Unit &u, int rows, 
       if (a.lse && part == 0) a.lse[t * (a.kv_heads * a.group) + hq] = lse_of(m, l);
     }
   } else {
-    float *to = a.part_o + (slot * 16 + row) * D + part * (D / 16);
+    const int64_t at = (slot * NT + tile) * 16 + row;
+    float *to = a.part_o + at * D + part * (D / 16);
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) to[c] = x[c];
     if (part == 0) {
-      a.part_ml[(slot * 16 + row) * 2] = m;
-      a.part_ml[(slot * 16 + row) * 2 + 1] = l;
+      a.part_ml[at * 2] = m;
+      a.part_ml[at * 2 + 1] = l;
     }
   }
 }
@@ -577,7 +563,7 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
     const Unit u = unit_at<16, SEL>(a, q, at, offset);
     const int n = a.whole ? u.pages : min(u.pages - offset, share.end - at);
     const int rows = min(16, u.fresh * a.group - u.tile * 16);
-    const Place<TREE> p = place_of<16, TREE>(a, u, rows, lane & 15);
+    const Place p = place_of<16, TREE>(a, u, rows, lane & 15);
     const int32_t *table = a.table + (int64_t)max(u.req, 0) * a.width;
     const int32_t *list = SEL ? a.selected + ((int64_t)u.t0 * a.kv_heads + u.head) * a.n_select : nullptr;
     const char *heads = a.pages + u.head * (int64_t)kv_head_bytes(D);
@@ -607,7 +593,7 @@ __global__ __launch_bounds__(256, 2) void kv_rows16_kernel(KvAttnArgs a) {
         const int first = __builtin_amdgcn_readlane(c, __builtin_ctzll(left)) * KV_PAGE;
         if (first + KV_PAGE > u.kv) pg.cut(u.kv - first, lane);
         const bool masked = first + KV_PAGE - 1 > p.clear_high || first <= p.clear_low;
-        const uint64_t sees = TREE && masked ? tree_sees<TREE>(a, p, first) : 0;
+        const uint64_t sees = TREE && masked ? tree_sees(a, u, p.t, p.low, first) : 0;
         page_step<D, DT, TREE>(pg, qf, r, lane, a.scale2, masked, first, p.low, p.high, sees);
       };
       // a page is requested while the one before it is worked on (256 channels: no registers for two)
@@ -767,7 +753,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, W
     const Unit u = unit_at<TR, false>(a, q, at, offset);
     const int n = a.whole ? u.pages : min(u.pages - offset, share.end - at);
     const int rows = min(TR, u.fresh * a.group - u.tile * TR);
-    Place<TREE> p[NQ];
+    Place p[NQ];
     u32x4 qf[NQ][C];
     Row<D> r[NQ];
 #pragma unroll
@@ -855,7 +841,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, W
 #pragma unroll
         for (int k = 0; k < NQ; ++k) {
           const bool masked = first + KV_PAGE - 1 > p[k].clear_high || first <= p[k].clear_low;
-          const uint64_t sees = TREE && masked ? tree_sees<TREE>(a, p[k], first) : 0;
+          const uint64_t sees = TREE && masked ? tree_sees(a, u, p[k].t, p[k].low, first) : 0;
           page_maximum<D, DT, TREE>(s[k], r[k], g, a.scale2, masked, first, p[k].low, p[k].high, 8.0f, sees);
         }
         read(4 * C, x[0]);
@@ -1103,6 +1089,15 @@ int attention_typed(const KvAttnArgs &a, int dtype, const Shape &sh, hipStream_t
   return dtype == IVFPQ_KV_BF16 ? attention_of<D, IVFPQ_KV_BF16, TREE>(a, sh, s) : attention_of<D, IVFPQ_KV_FP16, TREE>(a, sh, s);
 }
 
+void place_workspace(KvAttnArgs &a, const Shape &sh, char *workspace) {
+  a.n_wg = sh.n_wg;
+  a.whole = sh.whole;
+  a.prefix = reinterpret_cast<int32_t *>(workspace);
+  a.borders = reinterpret_cast<int32_t *>(workspace + sh.prefix);
+  a.part_ml = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders);
+  a.part_o = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders + sh.ml);
+}
+
 template <bool TREE>
 int launch_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s) {
   const Shape sh = shape_of(a.tokens, a.requests, a.kv_heads, a.group, D, max_new, a.window, a.selected ? a.n_select : 0,
@@ -1111,12 +1106,7 @@ int launch_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspac
     set_error("kv_attention: %d workgroups are too many for one launch", sh.n_wg);
     return IVFPQ_ERR_UNSUPPORTED;
   }
-  a.n_wg = sh.n_wg;
-  a.whole = sh.whole;
-  a.prefix = reinterpret_cast<int32_t *>(workspace);
-  a.borders = reinterpret_cast<int32_t *>(workspace + sh.prefix);
-  a.part_ml = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders);
-  a.part_o = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders + sh.ml);
+  place_workspace(a, sh, workspace);
   switch (D) {
     case 64: return attention_typed<64, TREE>(a, dtype, sh, s);
     case 96: return attention_typed<96, TREE>(a, dtype, sh, s);

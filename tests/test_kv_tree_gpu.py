@@ -212,6 +212,34 @@ def test_tree_rows_around_tile_borders(kv, n, G):
         s.attend_tree(2 * G)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("H,G,D", [(2, 4, 128), (2, 3, 64), (1, 5, 96), (1, 2, 256)])
+@pytest.mark.parametrize("new", [[9, 6, 13, 1, 8], [40, 3, 70, 16, 1]])
+@pytest.mark.parametrize("window", [0, 90])
+def test_trees_in_wide_tables(kv, dtype, H, G, D, new, window):
+    """Tables whose width promises long contexts decide how the work is cut: units of one and of two tiles, parts of them in shares, shares
+    across units and requests; a page in the middle of a request that is not there."""
+    rng = np.random.default_rng(D + G + len(new) + window)
+    s = TreeServer(kv, rng, dtype, H, D, 60, 5, 12000)
+    s.fill([700, 64, 5, 900, 333])
+    s.draft(new, window=window)
+    s.attend_tree(H * G, scale=-0.2)
+    s.d_table[3, 2] = s.want["table"][3, 2] = 60
+    s.d_table[0, 0] = s.want["table"][0, 0] = -1
+    s.attend_tree(H * G)
+
+
+@pytest.mark.parametrize("G,W", [(1, 4), (8, 4), (4, 100)])
+def test_trees_of_more_requests_than_are_scanned_in_a_workgroup(kv, G, W):
+    rng = np.random.default_rng(25)
+    R = 530
+    s = TreeServer(kv, rng, "bf16", 1, 64, 2 * R, R, W)
+    s.fill(rng.integers(0, 60, R))
+    s.draft(rng.integers(0, 7, R), max_tokens=7 * R)
+    s.attend_tree(G)
+    s.keep()
+
+
 @pytest.mark.parametrize("window", [1, 2, 7, 64, 100, 1000])
 @pytest.mark.parametrize("H,G,D,new", [(2, 2, 64, [9, 20, 3]), (1, 8, 128, [40, 70, 1])])
 def test_tree_windows(kv, window, H, G, D, new):
