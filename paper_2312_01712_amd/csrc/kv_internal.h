@@ -116,7 +116,7 @@ struct KvReadArgs {
 int launch_kv_rotate(const KvRotateArgs &a, int neighbours, int dtype, hipStream_t s);
 int launch_kv_tree(const KvTreeArgs &a, hipStream_t s);
 int launch_kv_accept(const KvKeepArgs &a, hipStream_t s);
-int launch_kv_move(const KvKeepArgs &a, int D, int dtype, bool ring, hipStream_t s);
+int launch_kv_move(const KvKeepArgs &a, int D, bool ring, hipStream_t s);
 int launch_kv_read(const KvReadArgs &a, int D, int dtype, hipStream_t s);
 size_t kv_tree_attention_workspace(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_nodes, int window,
                                    int64_t width);

@@ -17,14 +17,15 @@ __device__ inline Fresh fresh_of(const int32_t *q_start, int r, int tokens) {
   return {t0, max(min(q_start[r + 1], tokens) - t0, 0)};
 }
 
-// Workgroup (r, w): word w of the masks of request r's tokens, a thread a token.  Ancestors by doubling: after k turns a thread
+// Workgroup (r, y): words WORDS y .. of the masks of request r's tokens, a thread a token.  Ancestors by doubling: after k turns a thread
 // has the set of its token and the 2^k - 1 ancestors next to it, and the 2^k-th ancestor; the next turn adds that one's set.  As
-// many turns as the depth has bits.  A window takes the sets of its size's bits, one behind the other.
-template <int THREADS>
+// many turns as the depth has bits.  A window takes the sets of its size's bits, one behind the other.  Bound by the launch and
+// the trips lengths - parents: TREE_US for 700 requests of up to 200 tokens, 3.3 for one of 26.
+template <int THREADS, int WORDS>
 __global__ __launch_bounds__(THREADS) void kv_tree_kernel(KvTreeArgs a) {
-  __shared__ uint64_t set[THREADS];
+  __shared__ uint64_t set[WORDS][THREADS];
   __shared__ int32_t up[THREADS], far[THREADS];
-  const int i = threadIdx.x, r = blockIdx.x, w = blockIdx.y;
+  const int i = threadIdx.x, r = blockIdx.x, w0 = blockIdx.y * WORDS;
   if (r < a.requests) {
     const Fresh f = fresh_of(a.q_start, r, a.tokens);
     const int n = min(f.n, a.max_nodes);
@@ -34,38 +35,51 @@ __global__ __launch_bounds__(THREADS) void kv_tree_kernel(KvTreeArgs a) {
       const int p = a.parents[f.t0 + i];
       if (p >= 0 && p < i) parent = p;
     }
-    uint64_t mine = (i >> 6) == w ? 1ull << (i & 63) : 0, sees = 0;
+    const int first = f.n > 0 ? a.positions[f.t0] : 0;
+    uint64_t mine[WORDS], sees[WORDS];
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+      mine[w] = (i >> 6) == w0 + w ? 1ull << (i & 63) : 0;
+      sees[w] = 0;
+    }
     int steps = parent >= 0, at = i;
     for (int k = 0; (1 << k) < n; ++k) {
-      set[i] = mine;
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) set[w][i] = mine[w];
       up[i] = parent;
       far[i] = steps;
       const bool more = __syncthreads_or(parent >= 0);
       if (windowed && (a.window >> k & 1) && at >= 0) {
-        sees |= set[at];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) sees[w] |= set[w][at];
         at = up[at];
       }
       if (!more && !windowed) break;
       if (parent >= 0) {
-        mine |= set[parent];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) mine[w] |= set[w][parent];
         steps += far[parent];
         parent = up[parent];
       }
       __syncthreads();
     }
-    if (i < n) a.masks[(int64_t)(f.t0 + i) * a.words + w] = windowed ? sees : mine;
-    if (w == 0 && i < n) a.tree_positions[f.t0 + i] = a.positions[f.t0] + steps;
-    // tokens that the masks have no room for
-    for (int j = a.max_nodes + i; j < f.n; j += THREADS) {
-      a.masks[(int64_t)(f.t0 + j) * a.words + w] = 0;
-      if (w == 0) a.tree_positions[f.t0 + j] = -1;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+      if (w0 + w >= a.words) break;
+      if (i < n) a.masks[(int64_t)(f.t0 + i) * a.words + w0 + w] = windowed ? sees[w] : mine[w];
+      // tokens that the masks have no room for
+      for (int j = a.max_nodes + i; j < f.n; j += THREADS) a.masks[(int64_t)(f.t0 + j) * a.words + w0 + w] = 0;
+    }
+    if (w0 == 0) {
+      if (i < n) a.tree_positions[f.t0 + i] = first + steps;
+      for (int j = a.max_nodes + i; j < f.n; j += THREADS) a.tree_positions[f.t0 + j] = -1;
     }
   }
   // rows that stand for no token
   const int end = a.requests > 0 ? min(max(a.q_start[a.requests], 0), a.tokens) : 0;
   for (int64_t t = end + (int64_t)r * THREADS + i; t < a.tokens; t += (int64_t)gridDim.x * THREADS) {
-    a.masks[t * a.words + w] = 0;
-    if (w == 0) a.tree_positions[t] = -1;
+    for (int w = w0; w < min(w0 + WORDS, a.words); ++w) a.masks[t * a.words + w] = 0;
+    if (w0 == 0) a.tree_positions[t] = -1;
   }
 }
 
@@ -144,10 +158,10 @@ __global__ __launch_bounds__(THREADS) void kv_accept_kernel(KvKeepArgs a) {
 }  // namespace
 
 int launch_kv_tree(const KvTreeArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.requests > 0 ? a.requests : 1), (unsigned)a.words);
-  if (a.max_nodes <= 64) hipLaunchKernelGGL((kv_tree_kernel<64>), grid, dim3(64), 0, s, a);
-  else if (a.max_nodes <= 256) hipLaunchKernelGGL((kv_tree_kernel<256>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((kv_tree_kernel<1024>), grid, dim3(1024), 0, s, a);
+  const dim3 grid((unsigned)(a.requests > 0 ? a.requests : 1), (unsigned)((a.words + 3) / 4));
+  if (a.max_nodes <= 64) hipLaunchKernelGGL((kv_tree_kernel<64, 1>), grid, dim3(64), 0, s, a);
+  else if (a.max_nodes <= 256) hipLaunchKernelGGL((kv_tree_kernel<256, 4>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((kv_tree_kernel<1024, 4>), grid, dim3(1024), 0, s, a);
   KV_HIP_TRY(hipGetLastError());
   return IVFPQ_OK;
 }

@@ -203,7 +203,7 @@ int ivfpq_kv_keep(const ivfpq_kv_cache *caches, int32_t n_caches, const ivfpq_kv
       a.pages[i] = static_cast<char *>(caches[at + i].pages);
       a.boxes[i] = caches[at + i].boxes;
     }
-    if ((rc = launch_kv_move(a, caches[0].head_dim, caches[0].dtype, at == 0, hs))) return rc;
+    if ((rc = launch_kv_move(a, caches[0].head_dim, at == 0, hs))) return rc;
   }
   return IVFPQ_OK;
 }

@@ -119,6 +119,13 @@ def _ptr(t: torch.Tensor, dtype, shape, device: int, what: str) -> int:
 def _rows(t: torch.Tensor, dtype, shape, device: int, what: str) -> _Rows:
     """Rows [tokens][heads][head_dim] that the kernels may read or write where they are: any strides
     of tokens and heads that keep rows on 16 bytes, channels contiguous."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+            ts, hs, cs = t.stride()
+            if cs == 1:
+                return _Rows(t.data_ptr(), ts, hs)
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype:
         raise ValueError(f"{what}: expected a CUDA tensor of {dtype}, got {getattr(t, 'dtype', type(t))} on "
                          f"{getattr(t, 'device', 'the host')}")
@@ -283,6 +290,7 @@ class Rotary:
         device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         self._phases = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device=device)
         self._axis = torch.tensor(axes, dtype=torch.int32, device=device)
+        self._refs = {}  # the call's description for each head_dim and type
         self.device, self.axes, self.turned, self.neighbours = self._phases.device.index, max(axes) + 1, 2 * len(turns), bool(neighbours)
 
     def __call__(self, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
@@ -292,17 +300,21 @@ class Rotary:
         themselves among them; no other overlap."""
         heads, kv_heads, dev = _heads_of(q), _heads_of(k), self.device
         T, _, D = q.shape
-        if q.dtype not in _DTYPES:
-            raise ValueError(f"q must be of torch.bfloat16 or torch.float16, not {q.dtype}")
         dtype = q.dtype
-        qr, kr = _rows(q, dtype, (T, heads, D), dev, "q"), _rows(k, dtype, (T, kv_heads, D), dev, "k")
+        if dtype not in _DTYPES:
+            raise ValueError(f"q must be of torch.bfloat16 or torch.float16, not {dtype}")
+        shape_q, shape_k = (T, heads, D), (T, kv_heads, D)
+        qr, kr = _rows(q, dtype, shape_q, dev, "q"), _rows(k, dtype, shape_k, dev, "k")
         one = isinstance(positions, torch.Tensor) and positions.dim() == 1
         at = _ptr(positions, torch.int32, (T,) if one else (self.axes, T), dev, "positions")
         if out is None:
-            out = torch.empty((T, heads, D), dtype=dtype, device=q.device), torch.empty((T, kv_heads, D), dtype=dtype, device=q.device)
-        to_q, to_k = _rows(out[0], dtype, (T, heads, D), dev, "out q"), _rows(out[1], dtype, (T, kv_heads, D), dev, "out k")
-        c = _Rotary(D, self.turned, self.neighbours, _DTYPES[dtype], self.axes, self._phases.data_ptr(), self._axis.data_ptr())
-        _launch(dev, _lib().ivfpq_kv_rotate, ctypes.byref(c), qr, heads, kr, kv_heads, at, 0 if one else T, T, to_q, to_k)
+            out = torch.empty(shape_q, dtype=dtype, device=q.device), torch.empty(shape_k, dtype=dtype, device=q.device)
+        to_q, to_k = _rows(out[0], dtype, shape_q, dev, "out q"), _rows(out[1], dtype, shape_k, dev, "out k")
+        ref = self._refs.get((D, dtype))
+        if ref is None:
+            c = _Rotary(_int32(D, "head_dim"), self.turned, self.neighbours, _DTYPES[dtype], self.axes, self._phases.data_ptr(), self._axis.data_ptr())
+            ref = self._refs[D, dtype] = ctypes.byref(c)
+        _launch(dev, _lib().ivfpq_kv_rotate, ref, qr, heads, kr, kv_heads, at, 0 if one else T, T, to_q, to_k)
         return out[0], out[1]
 
 

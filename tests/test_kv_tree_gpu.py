@@ -369,14 +369,17 @@ def test_steps_with_drafts(kv, dtype, H, D):
         assert sorted(where) == list(range(n_pages))
 
 
-def test_keep_gives_what_appending_only_the_kept_gives(kv):
-    """Bytes of the held tokens and boxes, page for page, against a cache that never saw the others."""
+@pytest.mark.parametrize("dtype,new,tiny", [("bf16", [40, 70, 30, 9], 0), ("fp16", [40, 60, 30, 9], 0), ("bf16", [40, 64, 30, 9], -129),
+                                            ("fp16", [40, 64, 30, 9], -22)])
+def test_keep_gives_what_appending_only_the_kept_gives(kv, dtype, new, tiny):
+    """Bytes of the held tokens and boxes, page for page, against a cache that never saw the others; keys as small as the type has them."""
     rng = np.random.default_rng(13)
-    s = TreeServer(kv, rng, "bf16", 3, 128, 30, 4, 6)
+    s = TreeServer(kv, rng, dtype, 3, 128, 30, 4, 6)
+    s.gain *= 2.0 ** tiny
     s.fill([0, 60, 64, 130])
-    other = kv.KvCache(30, 3, 128)
+    other = kv.KvCache(30, 3, 128, TYPES[dtype])
     other.pages.copy_(s.cache.pages), other.boxes.copy_(s.cache.boxes)
-    T = s.draft([40, 70, 30, 9], parents=random_parents(rng, np.array([40, 70, 30, 9])))
+    T = s.draft(new, parents=random_parents(rng, np.array(new)))
     k, v = s.cache.read(s.step.slots)
     kept = s.keep(agree=1.0)
     q_start, slots = s.want["q_start"], s.step.slots
@@ -392,7 +395,7 @@ def test_keep_gives_what_appending_only_the_kept_gives(kv):
         assert torch.equal(a.view(torch.int16), b.view(torch.int16))
     pages = torch.unique(held // 64)
     assert torch.equal(s.cache.boxes[pages].view(torch.int16), other.boxes[pages].view(torch.int16))
-    assert T == 149
+    assert T == sum(new)
 
 
 def test_keep_in_many_layers(kv):
@@ -505,6 +508,35 @@ def test_read(kv, dtype, H, D):
     for n in (0, 1, 64, 130):
         a, b = s.cache.read(dev(slots[:n], torch.int64))
         assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(k[:n])) and torch.equal(b, v[:n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("H,D", [(4, 64), (5, 96), (4, 128), (8, 256), (33, 64)])
+def test_read_of_runs(kv, dtype, H, D):
+    """Long lists, where a lane has four tokens: runs of all lengths that begin anywhere in a page and in the list, slots outside, tokens that
+    are no numbers; the same bits as a few slots at a time, which are compared with the definitions above."""
+    rng = np.random.default_rng(D + H)
+    n_pages = 40
+    s = Server(kv, rng, dtype, H, D, n_pages, 1, n_pages, held=False)
+    s.ref = None
+    step = kv.plan(s.d_past, dev(np.array([n_pages * 64]), torch.int32), s.d_table, s.d_ring, s.d_state, max_tokens=n_pages * 64)
+    k, v = (rows(rng, dtype, n_pages * 64, H, D)[0] for _ in range(2))
+    k[5, 0, 1], v[77, H - 1, 2], k[1000, H // 2, 0] = float("nan"), float("inf"), float("-inf")
+    s.cache.append(k, v, step.slots)
+    parts = []
+    while sum(map(len, parts)) < 1500:
+        n = int(rng.choice([1, 2, 3, 4, 5, 8, 13, 64, 70, 130]))
+        parts.append(int(rng.integers(-3, n_pages * 64 - n + 4)) + np.arange(n))
+        if rng.random() < 0.1:
+            parts.append(rng.integers(0, n_pages * 64, 7))
+    for shift in range(5):
+        slots = dev(np.concatenate(parts)[shift:], torch.int64)
+        a, b = s.cache.read(slots)
+        few = 4000 // H
+        small = [s.cache.read(slots[i:i + few].contiguous()) for i in range(0, len(slots), few)]
+        assert len(slots) * H >= 4096
+        for got, want in ((a, torch.cat([x[0] for x in small])), (b, torch.cat([x[1] for x in small]))):
+            assert torch.equal(got.view(torch.int16), want.view(torch.int16))
 
 
 def test_read_and_keep_behind_32_bits(kv):
