@@ -279,8 +279,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D <= 128 ? 
   if (tid == 0 && !a.whole && share.begin >= share.end) a.borders[(int64_t)wg * BORDER_INTS] = 0;
   for (int at = share.begin; at < share.end;) {
     int offset;
-    const Unit u = unit_at<TR, false>(a, q, at, offset);
-    const int n = a.whole ? u.pages : min(u.pages - offset, share.end - at);
+    Unit u = unit_at<TR, false>(a, q, at, offset);
+    // entries of the unit: unit_extra, then its pages
+    const int extra = a.whole ? 0 : unit_extra<TR>(), entries = u.pages + extra;
+    const int taken = a.whole ? entries : min(entries - offset, share.end - at);
+    const int first = max(offset - extra, 0), n = max(offset + taken - extra, 0) - first;
     const int rows = min(TR, u.fresh * a.group - u.tile * TR);
     Row<D> r[NT];
 #pragma unroll
@@ -292,8 +295,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D <= 128 ? 
     }
     const int tiles = (rows + 15) / 16;
     char *place = lds + wave * (2 * half_bytes<D>());
-    if (tiles == 1) tiles_pages<D, DT, 1>(a, u, rows, offset, n, wave, lane, tid, in, place, r);
-    else tiles_pages<D, DT, NT>(a, u, rows, offset, n, wave, lane, tid, in, place, r);
+    if (tiles == 1) tiles_pages<D, DT, 1>(a, u, rows, first, n, wave, lane, tid, in, place, r);
+    else tiles_pages<D, DT, NT>(a, u, rows, first, n, wave, lane, tid, in, place, r);
 #pragma unroll
     for (int k = 0; k < NT; ++k)
       if (k < tiles) {
@@ -304,10 +307,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D <= 128 ? 
         for (int ct = 0; ct < D / 16; ++ct)
           *reinterpret_cast<f32x4 *>(buf + (wave * 16 + (lane & 15)) * (D + 4) + ct * 16 + g * 4) = r[k].o[ct];
         __syncthreads();
-        join_waves<D, DT, NT>(a, u, rows, n == u.pages, 2 * (int64_t)wg + (at != share.begin), ml, buf, tid, k);
+        join_waves<D, DT, NT>(a, u, rows, taken == entries, 2 * (int64_t)wg + (at != share.begin), ml, buf, tid, k);
       }
     __syncthreads();
-    const int next = at + (a.whole ? 1 : n);
+    const int next = at + (a.whole ? 1 : taken);
+    u.pages = entries;
     if (tid == 0 && !a.whole && next == share.end) leave_border(a, share, u, wg, at, rows);
     at = next;
   }
@@ -324,13 +328,15 @@ TreeShape tree_shape(int64_t tokens, int64_t requests, int kv_heads, int group, 
   const int64_t nodes = max_nodes < tokens ? max_nodes : tokens, rows = nodes * group;  // rows of a request and head, at most
   int64_t most = width;  // pages of a unit
   if (window > 0 && ((int64_t)window + nodes) / KV_PAGE + 2 < most) most = ((int64_t)window + nodes) / KV_PAGE + 2;
-  // 8 kv heads of 128, us.  16 rows and fewer: the kernel of decoding (32 requests of 4000 30, here 40).  Up to 64 rows: that one
-  // where there is little work, as its first page takes fewer trips (32 rows: one request of 8000 17, here 23; 32 of 1500 25 and
-  // 31; 64 rows of one of 8000 21 and 28), this one otherwise (32 rows: 16 of 16 000 97 and 82; 64 rows: 32 of 1500 44 and 38, one of
-  // 100 000 74 and 64, 16 of 16 000 168 and 125).  More rows: the kernels of chunks (128 rows: 32 of 4000 116 and 128; 256: 152
-  // and 222), this one where there is little work (128 rows: one of 500 19 and 13, of 8000 35 and 31; 512 of 8000 48 and 43).
+  // 8 kv heads of 128, us.  16 rows and fewer: the kernel of decoding (32 requests of 4000 30, here 40).  Little work: that one up to
+  // 64 rows, as its first page takes fewer trips (32 rows: one request of 8000 17, here 23; 32 of 1500 25 and 31; 64 rows of one of
+  // 8000 21 and 28), this one beyond (128 rows: one of 500 19 in the kernel of chunks and here 13, of 8000 35 and 31).  Otherwise
+  // this one up to 96 rows (32: 16 of 16 000 98 and 82; 64: the same 168 and 117; 96: 32 of 4000 106 and 81), the
+  // kernels of chunks beyond (128: 32 of 4000 113 and 129; 256: 152 and 222), but where requests have fewer tokens than the largest,
+  // whose tiles they leave part empty (64 of up to 8000, trees of up to 128 rows 147 and 101, 512 365 and 286).
   const bool little = ((tokens * group + 15) / 16 + requests) * kv_heads * most < 32768;
-  s.tiles = rows <= 16 ? 0 : (rows <= 64) != little ? NT : 0;
+  const bool ragged = tokens * 8 <= requests * nodes * 7;
+  s.tiles = rows <= 16 ? 0 : little ? (rows > 64 ? NT : 0) : rows <= 96 || (ragged && rows <= 512) ? NT : 0;
   if (s.tiles == 0) {
     static_cast<Shape &>(s) = shape_of(tokens, requests, kv_heads, group, D, max_nodes, window, 0, width);
     return s;
@@ -340,7 +346,7 @@ TreeShape tree_shape(int64_t tokens, int64_t requests, int kv_heads, int group, 
   const int64_t units = (tokens * group / s.tile_rows + requests) * kv_heads;
   const int fill = D <= 128 ? 768 : 256;
   const int64_t surely = window > 0 ? (window + tokens) / KV_PAGE + 2 : width;
-  s.whole = narrow || units * (surely < width ? surely : width) > 0x7fffffff;
+  s.whole = narrow || units * ((surely < width ? surely : width) + UNIT_EXTRA) > 0x7fffffff;
   const int shares = units * most / 4 >= fill ? fill : (int)(units * most / 4 + 1);
   s.n_wg = s.whole ? (int)units : shares;
   if (s.n_wg < 1) s.n_wg = 1;
