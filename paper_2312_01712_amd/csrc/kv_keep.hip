@@ -110,7 +110,8 @@ struct Box {
 // 4-bit codes still, so these are the boxes that appending only them would have given); then what stays moves to lower slots in the
 // order of tokens, four at a time: what a later one comes from lies behind everything written.  SMALL: no request has more than 64
 // new tokens, a lane each, which takes three trips to memory before the first write.  Bound by these trips: 48 requests of up to
-// 64 drafted tokens, 8 heads of 128, 28 caches, 43 MB, KEEP_US.
+// 64 drafted tokens, 8 heads of 128, 28 caches, 43 MB, 25 us (keys from memory into boxes one value at a time, behind the moves, 34);
+// one request, 4 caches, 6.7.
 template <int D, bool SMALL>
 __global__ __launch_bounds__(256) void kv_move_kernel(KvKeepArgs a, int ring) {
   constexpr int BYTES = 68 * D / 64, TRIPS = (BYTES + 63) / 64, AHEAD = 4;
@@ -252,7 +253,9 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvKeepArgs a, int ring) {
   }
 }
 
-constexpr int READ_RUNS = 4096;  // tokens times heads from which on a lane has four tokens
+// Tokens times heads from which on a lane has four tokens (8 heads of 128, us, a token a lane and four: runs of 64, 1024 tokens 4.8 and
+// 4.4, 2048 7.0 and 5.0, 16 384 37 and 17; from everywhere 1024 4.8 and 8.0, 2048 7.6 and 9.5, 16 384 38 and 39).
+constexpr int READ_RUNS = 16384;
 
 // Eight channels of a held token's keys and values.
 template <int D, int DT>
@@ -269,7 +272,7 @@ __device__ inline void read_token(const char *at, int place, int oct, u32x4 &k, 
   v = held_row<DT>(vc, vb);
 }
 
-// D / 8 lanes have a token and head, eight channels each.
+// D / 8 lanes have a token and head, eight channels each.  301 tokens of 8 heads of 64: 3.6 us, the launch and two trips.
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvReadArgs a) {
   constexpr int OCT = D / 8;
@@ -286,21 +289,22 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvReadArgs a) {
 }
 
 // Four tokens a lane.  A page has four tokens' values of a channel beside each other, so four that follow each other, from a multiple
-// of four on, take the loads of one; the fours of a workgroup's 64 tokens begin where its first token says.
+// of four on, take the loads of one; the fours of a workgroup's 64 tokens begin where its first token says.  Bound by memory: 30 011
+// tokens of 8 heads of 128, 34 MB read (pages that come twice once) and 123 written, 36 us (4.3 TB/s); a token a lane 65.
 template <int D, int DT>
 __global__ __launch_bounds__(256) void kv_read_run_kernel(KvReadArgs a, int heads_at_once) {
   constexpr int OCT = D / 8, TILE = 64;
   const int64_t begin = (int64_t)blockIdx.x * TILE, end = min(begin + TILE, a.tokens);
   const int h0 = blockIdx.y * heads_at_once, heads = min(heads_at_once, a.kv_heads - h0);
   const int64_t ahead = a.slots[begin];
-  const int shift = ahead >= 0 ? (int)(ahead & 3) : 0;
-  for (int i = threadIdx.x; i < (TILE / 4 + 1) * heads * OCT; i += 256) {
+  const int shift = ahead >= 0 && begin + 1 < end && a.slots[begin + 1] == ahead + 1 ? (int)(ahead & 3) : 0;
+  for (int i = threadIdx.x; i < (TILE / 4 + (shift != 0)) * heads * OCT; i += 256) {
     const int oct = i % OCT, rest = i / OCT, h = h0 + rest % heads, group = oct >> 2;
     const int64_t t0 = begin - shift + rest / heads * 4;
     if (t0 >= end) continue;
     int64_t slot[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) slot[j] = t0 + j >= begin && t0 + j < end ? a.slots[t0 + j] : -2;
+    for (int j = 0; j < 4; ++j) slot[j] = t0 + j >= begin && t0 + j < end ? a.slots[t0 + j] : -1;
     uint16_t *to_k = a.k + t0 * a.k_token + h * a.k_head + oct * 8, *to_v = a.v + t0 * a.v_token + h * a.v_head + oct * 8;
     if (slot[0] >= 0 && (slot[0] & 3) == 0 && slot[0] < a.n_slots && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 && slot[3] == slot[0] + 3) {
       const int place = (int)(slot[0] % KV_PAGE), lane = ((place >> 2) & 3) * 16, word = (place >> 4) * 4;
@@ -325,13 +329,20 @@ __global__ __launch_bounds__(256) void kv_read_run_kernel(KvReadArgs a, int head
         *reinterpret_cast<u32x4 *>(to_v + j * a.v_token) = held_row<DT>(vc, vb >> (8 * j) & 0xff);
       }
     } else {
+      // (all four tokens' loads before the first store; a token that is not there reads the cache's first)
+      u32x4 k[4], v[4];
+#pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (slot[j] == -2 && (t0 + j < begin || t0 + j >= end)) continue;
-        u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-        if (slot[j] >= 0 && slot[j] < a.n_slots)
-          read_token<D, DT>(a.pages + (slot[j] / KV_PAGE * a.kv_heads + h) * (int64_t)kv_head_bytes(D), (int)(slot[j] % KV_PAGE), oct, k, v);
-        *reinterpret_cast<u32x4 *>(to_k + j * a.k_token) = k;
-        *reinterpret_cast<u32x4 *>(to_v + j * a.v_token) = v;
+        const bool inside = slot[j] >= 0 && slot[j] < a.n_slots;
+        const int64_t from = inside ? slot[j] : 0;
+        read_token<D, DT>(a.pages + (from / KV_PAGE * a.kv_heads + h) * (int64_t)kv_head_bytes(D), (int)(from % KV_PAGE), oct, k[j], v[j]);
+        if (!inside) k[j] = v[j] = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (t0 + j < begin || t0 + j >= end) continue;
+        *reinterpret_cast<u32x4 *>(to_k + j * a.k_token) = k[j];
+        *reinterpret_cast<u32x4 *>(to_v + j * a.v_token) = v[j];
       }
     }
   }

@@ -3,7 +3,7 @@
 //
 // Angles are counted in turns, as 64-bit fractions of one: frequency / 2 pi times 2^64, times a whole position, modulo 2^64, is
 // the exact fraction of a turn whatever the position (in 32 bits a position of 10^6 would leave an angle 0.06 off).  Its
-// upper 32 bits go to the hardware's sine and cosine, which take turns.
+// upper 32 bits go to the hardware's sine and cosine, which take turns (2^-22.9 off at most, over 2^20 turns from -1/2 to 1/2).
 
 #include "kv_internal.h"
 
@@ -22,7 +22,7 @@ __device__ inline void turn_of(int32_t position, uint64_t phase, float &c, float
 }
 
 // A thread has 16 channels (8 pairs, or 16 that are not turned) of every slots-th head of a token, so that it computes its
-// sines once.
+// sines once for them.  Bound by memory: 9001 tokens of 40 heads of 128, 184 MB, 41 us (4.5 TB/s); one of 24 heads 2.4 us.
 template <int D, int DT, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void kv_rotate_kernel(KvRotateArgs a) {
   constexpr int CHUNKS = D / 16;
@@ -89,8 +89,9 @@ void rotate_typed(const KvRotateArgs &a, int neighbours, int dtype, unsigned gri
 int launch_kv_rotate(const KvRotateArgs &args, int neighbours, int dtype, hipStream_t s) {
   KvRotateArgs a = args;
   const int64_t total = a.heads + (int64_t)a.kv_heads, chunks = a.dim / 16, all = a.tokens * total * chunks;
-  int64_t per = all / (256 * 1024);
-  per = per < 1 ? 1 : per > 8 ? 8 : per;
+  // two heads a thread where there are threads enough (40 heads of 128, us, one head a thread, two, four, eight: one token 3.2, 3.3, 3.9,
+  // 4.7; 256 4.1, 3.9, 4.6, 5.9; 1024 6.4, 6.0, 6.1, 6.7; 9000 31.7, 30.6, 30.9, 32.2)
+  const int64_t per = all >= 65536 ? 2 : 1;
   a.slots = (int32_t)((total + per - 1) / per);
   const int64_t threads = a.tokens * a.slots * chunks;
   if (!launch_fits((threads + 255) / 256, 256)) {

@@ -246,11 +246,12 @@ __device__ inline void tiles_pages(const KvAttnArgs &a, const Unit &u, int rows,
 }
 
 // Units of up to NT tiles, shared out among workgroups as in kv_rows16_kernel; a workgroup's four wavefronts take a unit's pages in
-// turn and add up through LDS.  Bound by the issue of instructions: a page and two tiles are 530 of the vector units, a third of
-// them unpacking, and 64 products, which together take 2600 cycles of a SIMD; 16 tokens of 32 heads behind 300 001, 79 GFLOP, 328 MB,
-// 128 us and 10 of joining (16 rows a tile as in decoding: 168 in all; three tiles, two wavefronts a SIMD: 160; four tiles, which have no
-// registers for a second wavefront: 155).  Scaled products of the 4-bit codes themselves would save unpacking keys, but sum to 2^-17
-// of the sizes' sum only, and take no 16-bit queries.
+// turn and add up through LDS.  Bound by the issue of instructions (vector units 53 % busy, matrix units 23 %, and a product takes the
+// issue of seven cycles): a page and two tiles are 420 instructions of the vector units, half of them unpacking, and 64 products.  16
+// tokens of 32 heads behind 300 001, 79 GFLOP, 328 MB, 117 us and 10 of joining (16 rows a tile as in decoding: 168 in all); trees
+// of up to 32 tokens, 64 heads, behind 24 contexts to 33 000, 117 GFLOP, 190 us (in the kernel of chunks 245).  Three tiles with two
+// wavefronts a SIMD took 160 and 282 us, four, which leave a few values to memory in the loop, 169 and 328.  Scaled products of the 4-bit
+// codes themselves would save unpacking keys, but sum to 2^-17 of the sizes' sum only, and take no 16-bit queries.
 template <int D, int DT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D <= 128 ? 3 : 2))) void kv_tiles_kernel(KvAttnArgs a) {
   constexpr int TR = 16 * NT;
@@ -321,6 +322,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D <= 128 ? 
 // How a call is cut.  tiles: of 16 rows that a wavefront has, or 0 for the kernels of chunks.
 struct TreeShape : Shape {
   int tiles;
+  int64_t units;
 };
 
 TreeShape tree_shape(int64_t tokens, int64_t requests, int kv_heads, int group, int D, int max_nodes, int window, int64_t width) {
@@ -343,7 +345,7 @@ TreeShape tree_shape(int64_t tokens, int64_t requests, int kv_heads, int group, 
   }
   const bool narrow = most <= WHOLE_PAGES;
   s.tile_rows = 16 * s.tiles;
-  const int64_t units = (tokens * group / s.tile_rows + requests) * kv_heads;
+  const int64_t units = s.units = (tokens * group / s.tile_rows + requests) * kv_heads;
   const int fill = D <= 128 ? 768 : 256;
   const int64_t surely = window > 0 ? (window + tokens) / KV_PAGE + 2 : width;
   s.whole = narrow || units * ((surely < width ? surely : width) + UNIT_EXTRA) > 0x7fffffff;
@@ -373,7 +375,15 @@ int tiles_of(KvAttnArgs a, const TreeShape &sh, hipStream_t s) {
   if (a.whole || a.n_wg == 1) return IVFPQ_OK;
   const int64_t most = a.tokens * (int64_t)a.group;
   const int rows = (int)(most < sh.tile_rows ? most : sh.tile_rows);
-  hipLaunchKernelGGL((kv_join_kernel<D, DT, true>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a, sh.tile_rows);
+  // few units of dozens of parts each: a workgroup a row; many of two or three: a workgroup 256 / (D / 4) rows (800 units
+  // over 768 shares: 21 us and 7)
+  if (sh.n_wg >= 8 * sh.units) {
+    hipLaunchKernelGGL((kv_join_kernel<D, DT, true>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a, sh.tile_rows);
+  } else {
+    constexpr int SETS = 256 / (D / 4);
+    hipLaunchKernelGGL((kv_join_kernel<D, DT, false>), dim3((unsigned)(a.n_wg - 1), (unsigned)((rows + SETS - 1) / SETS)), dim3(256), 0, s, a,
+                       sh.tile_rows);
+  }
   KV_HIP_TRY(hipGetLastError());
   return IVFPQ_OK;
 }
