@@ -110,10 +110,10 @@ struct Box {
 // 4-bit codes still, so these are the boxes that appending only them would have given); then what stays moves to lower slots in the
 // order of tokens, four at a time: what a later one comes from lies behind everything written.  SMALL: no request has more than 64
 // new tokens, a lane each, which takes three trips to memory before the first write.  Bound by these trips: 48 requests of up to
-// 64 drafted tokens, 8 heads of 128, 28 caches, 43 MB, 25 us (keys from memory into boxes one value at a time, behind the moves, 34);
+// 64 drafted tokens, 8 heads of 128, 28 caches, 43 MB, 23 us (the boxes behind the moves, a value at a time, 34);
 // one request, 4 caches, 6.7.
 template <int D, bool SMALL>
-__global__ __launch_bounds__(256) void kv_move_kernel(KvKeepArgs a, int ring) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 5 : 8))) void kv_move_kernel(KvKeepArgs a, int ring) {
   constexpr int BYTES = 68 * D / 64, TRIPS = (BYTES + 63) / 64, AHEAD = 4;
   constexpr int OCT = D / 8, TOKENS = 64 / OCT, TRIP = 8;  // lanes of a token's keys, tokens at a time, of which so many on their way
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
