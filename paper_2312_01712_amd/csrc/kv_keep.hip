@@ -111,13 +111,16 @@ struct Box {
 // order of tokens, four at a time: what a later one comes from lies behind everything written.  SMALL: no request has more than 64
 // new tokens, a lane each, which takes three trips to memory before the first write.  Bound by these trips: 48 requests of up to
 // 64 drafted tokens, 8 heads of 128, 28 caches, 43 MB, 23 us (the boxes behind the moves, a value at a time, 34);
-// one request, 4 caches, 6.7.
+// one request, 4 caches, 6.4 (the moves behind the boxes, the ring by the first workgroups, 6.7).
 template <int D, bool SMALL>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 5 : 8))) void kv_move_kernel(KvKeepArgs a, int ring) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 4 : 7))) void kv_move_kernel(KvKeepArgs a) {
   constexpr int BYTES = 68 * D / 64, TRIPS = (BYTES + 63) / 64, AHEAD = 4;
   constexpr int OCT = D / 8, TOKENS = 64 / OCT, TRIP = 8;  // lanes of a token's keys, tokens at a time, of which so many on their way
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x;
-  if (ring && blockIdx.y == 0 && blockIdx.z == 0) give_back(a, r, tid);
+  if ((int)blockIdx.z == a.n_caches) {  // behind the caches: the ring
+    if (blockIdx.y == 0) give_back(a, r, tid);
+    return;
+  }
   const int h = blockIdx.y * 4 + wave;
   if (r >= a.requests || h >= a.kv_heads) return;
   const int t0 = min(max(a.q_start[r], 0), a.tokens), n = min(a.q_start[r + 1], a.tokens) - t0, kv = a.kv_lens[r], stays = a.lens[r];
@@ -166,6 +169,38 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 5
     const int64_t to = target(i);
     return (uint64_t)from < n_slots && (uint64_t)to < n_slots ? from : to;
   };
+
+  // four tokens' bytes, from where they are to where they go; the first four are on their way while the boxes are made
+  int kind[TRIPS], base[TRIPS];
+#pragma unroll
+  for (int m = 0; m < TRIPS; ++m) kind[m] = byte_kind<D>(m * 64 + lane), base[m] = byte_base<D>(m * 64 + lane);
+  uint8_t x[AHEAD][TRIPS];
+  int64_t to[AHEAD];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int i = min(i0 + j, kept - 1);
+      const int64_t from = source(i);
+      to[j] = target(i);
+      if (i0 + j >= kept || from == to[j]) to[j] = -1;  // (also where one of the two is nowhere)
+      if (to[j] < 0) continue;
+      const char *at = pages + (from >> 6) * page_bytes;
+#pragma unroll
+      for (int m = 0; m < TRIPS; ++m)
+        if (m * 64 + lane < BYTES) x[j][m] = *reinterpret_cast<const uint8_t *>(at + base[m] + byte_place<D>(kind[m], (int)from & 63));
+    }
+  };
+  auto store = [&]() {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (to[j] < 0) continue;
+      char *at = pages + (to[j] >> 6) * page_bytes;
+#pragma unroll
+      for (int m = 0; m < TRIPS; ++m)
+        if (m * 64 + lane < BYTES) *reinterpret_cast<uint8_t *>(at + base[m] + byte_place<D>(kind[m], (int)to[j] & 63)) = x[j][m];
+    }
+  };
+  load(in_place);
 
   const int sub = lane / OCT, oct = lane % OCT;
   for (int c = first_column; c < end_column; ++c) {
@@ -223,33 +258,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 5
     }
   }
 
-  int kind[TRIPS], base[TRIPS];
-#pragma unroll
-  for (int m = 0; m < TRIPS; ++m) kind[m] = byte_kind<D>(m * 64 + lane), base[m] = byte_base<D>(m * 64 + lane);
-  for (int i0 = in_place; i0 < kept; i0 += AHEAD) {
-    uint8_t x[AHEAD][TRIPS];
-    int64_t to[AHEAD];
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      const int i = min(i0 + j, kept - 1);
-      const int64_t from = source(i);
-      to[j] = target(i);
-      if (i0 + j >= kept || from == to[j]) to[j] = -1;  // (also where one of the two is nowhere)
-      if (to[j] < 0) continue;
-      const char *at = pages + (from >> 6) * page_bytes;
-#pragma unroll
-      for (int m = 0; m < TRIPS; ++m)
-        if (m * 64 + lane < BYTES) x[j][m] = *reinterpret_cast<const uint8_t *>(at + base[m] + byte_place<D>(kind[m], (int)from & 63));
-    }
+  wave_fence();
+  store();
+  for (int i0 = in_place + AHEAD; i0 < kept; i0 += AHEAD) {
     wave_fence();
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      if (to[j] < 0) continue;
-      char *at = pages + (to[j] >> 6) * page_bytes;
-#pragma unroll
-      for (int m = 0; m < TRIPS; ++m)
-        if (m * 64 + lane < BYTES) *reinterpret_cast<uint8_t *>(at + base[m] + byte_place<D>(kind[m], (int)to[j] & 63)) = x[j][m];
-    }
+    load(i0);
+    wave_fence();
+    store();
   }
 }
 
@@ -371,9 +386,9 @@ int read_of(const KvReadArgs &a, int dtype, hipStream_t s) {
 
 template <int D>
 void move_of(const KvKeepArgs &a, int ring, hipStream_t s) {
-  const dim3 grid((unsigned)(a.requests > 0 ? a.requests : 1), (unsigned)((a.kv_heads + 3) / 4), (unsigned)a.n_caches);
-  if (a.max_nodes <= 64) hipLaunchKernelGGL((kv_move_kernel<D, true>), grid, dim3(256), 0, s, a, ring);
-  else hipLaunchKernelGGL((kv_move_kernel<D, false>), grid, dim3(256), 0, s, a, ring);
+  const dim3 grid((unsigned)(a.requests > 0 ? a.requests : 1), (unsigned)((a.kv_heads + 3) / 4), (unsigned)(a.n_caches + ring));
+  if (a.max_nodes <= 64) hipLaunchKernelGGL((kv_move_kernel<D, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((kv_move_kernel<D, false>), grid, dim3(256), 0, s, a);
 }
 
 }  // namespace
