@@ -262,18 +262,32 @@ struct Requests {
   int32_t *t0, *kv, *pos0;    // in LDS, or null: read from the step's arrays
 };
 
-// What a unit counts beside its pages where it is shared out: in units of two tiles, whose workgroups may have many small ones, about as
-// many pages as finding, placing and joining it takes (24 trees of up to 32 tokens, 64 heads, behind up to 33 000: 247 us
-// without, 215 with 6, 220 with 12).
-template <int TR>
-constexpr int unit_extra() { return TR == 32 ? UNIT_EXTRA : 0; }
+// Units of up to 64 rows in tiles (TILES): what an index counts.  With up to 32 rows a workgroup's four wavefronts take four pages at a time,
+// with more, two: a page counts for as much time.  Beside its pages a unit counts about as many as finding, placing and joining
+// it takes (in units of 32 rows, 24 trees of up to 32 tokens, 64 heads, behind up to 33 000: 247 us without, 215 with 6, 220 with 12).
+__device__ inline int unit_weight(int rows) { return rows > 32 ? 2 : 1; }
+
+struct TileUnits {
+  int64_t rows;
+  int tiles, full, last, head;  // units of a head, indexes of a unit of 64 rows, of the last one, of a head
+};
+__device__ inline TileUnits tile_units(int64_t rows, int pages, bool whole) {
+  TileUnits t;
+  t.rows = rows;
+  t.tiles = (int)((rows + 63) / 64);
+  t.full = whole ? 1 : 2 * (pages + UNIT_EXTRA);
+  t.last = whole ? 1 : unit_weight((int)(rows - 64 * (int64_t)(t.tiles - 1))) * (pages + UNIT_EXTRA);
+  t.head = (t.tiles - 1) * t.full + t.last;
+  return t;
+}
 
 // Whole units are counted instead of their pages.  The host sees to it that all of them stay below 2^31.
-template <int TR>
+template <int TR, bool TILES>
 __device__ inline int units_of(const KvAttnArgs &a, int fresh, int kv) {
   if (fresh <= 0) return 0;
+  if constexpr (TILES) return a.kv_heads * tile_units((int64_t)fresh * a.group, request_pages(kv, fresh, a.window, a.width).n, a.whole).head;
   const int n = (int)(((int64_t)fresh * a.group + TR - 1) / TR) * a.kv_heads;
-  return a.whole ? n : n * (request_pages(kv, fresh, a.window, a.width).n + unit_extra<TR>());
+  return a.whole ? n : n * request_pages(kv, fresh, a.window, a.width).n;
 }
 
 // Position of a request's first new token.  Where the table's width has cut the request its length does not say.
@@ -283,7 +297,7 @@ __device__ inline int first_position(const KvAttnArgs &a, int t0, int fresh, int
 }
 
 // Units before every request, by the whole workgroup; returns their sum.
-template <int TR, int THREADS>
+template <int TR, int THREADS, bool TILES = false>
 __device__ inline int scan_units(const KvAttnArgs &a, const Requests &q, int *sums, int tid) {
   const int lane = tid & 63, wave = tid >> 6;
   int carry = 0;
@@ -292,7 +306,7 @@ __device__ inline int scan_units(const KvAttnArgs &a, const Requests &q, int *su
     int n = 0;
     if (r < a.requests) {
       const int t0 = a.q_start[r], fresh = min(a.q_start[r + 1], a.tokens) - t0, kv = a.kv_lens[r];
-      n = units_of<TR>(a, fresh, kv);
+      n = units_of<TR, TILES>(a, fresh, kv);
       if (q.t0) {
         q.t0[r] = t0;
         q.kv[r] = kv;
@@ -312,11 +326,11 @@ __device__ inline int scan_units(const KvAttnArgs &a, const Requests &q, int *su
   return uniform(carry);
 }
 
-__global__ __launch_bounds__(1024) void kv_scan_kernel(KvAttnArgs a, int tile_rows) {
+__global__ __launch_bounds__(1024) void kv_scan_kernel(KvAttnArgs a, int tile_rows, int tiles) {
   __shared__ int sums[16];
   const Requests q = {a.prefix, nullptr, nullptr, nullptr};
-  const int total = tile_rows == 16 ? scan_units<16, 1024>(a, q, sums, threadIdx.x)
-                      : tile_rows == 32 ? scan_units<32, 1024>(a, q, sums, threadIdx.x)
+  const int total = tiles ? scan_units<64, 1024, true>(a, q, sums, threadIdx.x)
+                      : tile_rows == 16 ? scan_units<16, 1024>(a, q, sums, threadIdx.x)
                       : tile_rows == 64 ? scan_units<64, 1024>(a, q, sums, threadIdx.x)
                       : tile_rows == 128 ? scan_units<128, 1024>(a, q, sums, threadIdx.x)
                                          : scan_units<256, 1024>(a, q, sums, threadIdx.x);
@@ -324,7 +338,7 @@ __global__ __launch_bounds__(1024) void kv_scan_kernel(KvAttnArgs a, int tile_ro
 }
 
 // The unit that index `at` belongs to, and which of its pages that is.
-template <int TR, bool SEL>
+template <int TR, bool SEL, bool TILES = false>
 __device__ inline Unit unit_at(const KvAttnArgs &a, const Requests &q, int at, int &offset) {
   Unit u;
   int k;  // unit of its group
@@ -360,11 +374,18 @@ __device__ inline Unit unit_at(const KvAttnArgs &a, const Requests &q, int at, i
       u.pos0 = uniform(first_position(a, u.t0, u.fresh, u.kv));
     }
     const Range pr = request_pages(u.kv, u.fresh, a.window, a.width);
-    const int tiles = (int)(((int64_t)u.fresh * a.group + TR - 1) / TR), n = a.whole ? 1 : pr.n + unit_extra<TR>();
     const int rest = at - uniform(q.prefix[lo]);
-    k = rest / n;
-    offset = rest % n;
-    u.head = k / tiles, u.tile = k % tiles;
+    if constexpr (TILES) {
+      const TileUnits t = tile_units((int64_t)u.fresh * a.group, pr.n, a.whole);
+      u.head = rest / t.head;
+      u.tile = min(rest % t.head / t.full, t.tiles - 1);
+      offset = rest % t.head - u.tile * t.full;
+    } else {
+      const int tiles = (int)(((int64_t)u.fresh * a.group + TR - 1) / TR), n = a.whole ? 1 : pr.n;
+      k = rest / n;
+      offset = rest % n;
+      u.head = k / tiles, u.tile = k % tiles;
+    }
     u.lo = pr.lo, u.pages = pr.n;
   }
   u.first = at - offset;
@@ -473,19 +494,19 @@ __device__ inline float lse_of(float m, float l) {
   return l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
 
-// A unit's rows from the four wavefronts that had some of its pages each: to the result, or to the workspace.
+// A unit's rows from the wavefronts that had some of its pages each: to the result, or to the workspace.
 // tile: which 16 of a unit of NT tiles.
-template <int D, int DT, int NT = 1>
+template <int D, int DT, int NT = 1, int WAVES = 4>
 __device__ inline void join_waves(const KvAttnArgs &a, const Unit &u, int rows, bool whole, int64_t slot, float (*ml)[16][2],
                                   float *buf, int tid, int tile = 0) {
-  // buf [4][16][D + 4], ml [4]
+  // buf [WAVES][16][D + 4], ml [WAVES]
   const int row = tid >> 4, part = tid & 15;
-  float m = -__builtin_inff(), l = 0.0f, f[4];
+  float m = -__builtin_inff(), l = 0.0f, f[WAVES];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w][row][0]);
+  for (int w = 0; w < WAVES; ++w) m = fmaxf(m, ml[w][row][0]);
   const float base = m == -__builtin_inff() ? 0.0f : m;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     f[w] = __builtin_amdgcn_exp2f(ml[w][row][0] - base);
     l += f[w] * ml[w][row][1];
   }
@@ -494,7 +515,7 @@ __device__ inline void join_waves(const KvAttnArgs &a, const Unit &u, int rows, 
   for (int c = 0; c < D / 16; ++c) {
     x[c] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) x[c] += f[w] * buf[(w * 16 + row) * (D + 4) + part * (D / 16) + c];
+    for (int w = 0; w < WAVES; ++w) x[c] += f[w] * buf[(w * 16 + row) * (D + 4) + part * (D / 16) + c];
   }
   if (whole) {
     if (tile * 16 + row < rows) {
@@ -915,23 +936,49 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, W
   clear_rest<D, THREADS>(a, wg, gridDim.x, tid);
 }
 
+// The share that leaves the i-th unit across its border, -1: there are fewer; by the workgroup's 256 threads.
+__device__ inline int border_at(const KvAttnArgs &a, int shares, int i, int tid) {
+  __shared__ int sums[4], found;
+  const int lane = tid & 63, wave = tid >> 6, per = (shares + 255) / 256, first = tid * per, end = min(first + per, shares);
+  if (tid == 0) found = -1;
+  int own = 0;
+#pragma unroll 4
+  for (int j = first; j < end; ++j) own += a.borders[(int64_t)j * BORDER_INTS] != 0;
+  int x = lanes_up_to(own);
+  if (lane == 63) sums[wave] = x;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) x += sums[w];
+  if (i >= x - own && i < x) {
+    int left = i - (x - own);
+    for (int j = first; j < end; ++j)
+      if (a.borders[(int64_t)j * BORDER_INTS] != 0 && left-- == 0) found = j;
+  }
+  __syncthreads();
+  return uniform(found);
+}
+
 // Units that several workgroups share.  Workgroup (w, y) adds up the parts of ROWS rows of the unit that goes across
 // the border behind share w and began in it.  D / 4 lanes have a part (ROWS = 1) or a row each: decode has one
 // tile of few rows and up to all shares in a unit (520 001 tokens, 64 shares a unit: 40 us with a thread a row
 // and 8 channels, now 5), chunks have many rows of few parts (a workgroup a row there: 29 us for 256 shares).
 template <int D, int DT, bool ONE>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a, int tile_rows) {
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a, int tile_rows, int shares) {
   constexpr int LANES = D / 4, SETS = 256 / LANES;  // 96 channels: 24 lanes, 10 sets, 16 threads idle
   __shared__ float red_m[4];
   __shared__ f32x4 red_o[ONE ? SETS : 1][LANES];
   __shared__ float red_l[SETS];
   const int tid = threadIdx.x, set = tid / LANES, lane = tid % LANES;
   const int row = ONE ? blockIdx.y : blockIdx.y * SETS + set;
-  const int32_t *b = a.borders + (int64_t)blockIdx.x * BORDER_INTS;
+  int border = blockIdx.x;
+  if constexpr (ONE) {
+    if (shares > 0) border = border_at(a, shares, border, tid);
+    if (border < 0) return;
+  }
+  const int32_t *b = a.borders + (int64_t)border * BORDER_INTS;
   const int n = b[0], late = b[1], t0 = b[2], tile = b[3], head = b[4], rows = b[5];
   if (n == 0 || (ONE ? row : (int)blockIdx.y * SETS) >= rows) return;
   // a workgroup's first unit is in its slot 0
-  auto slot = [&](int k) { return 2 * ((int64_t)blockIdx.x + k) + (k == 0 && late); };
+  auto slot = [&](int k) { return 2 * ((int64_t)border + k) + (k == 0 && late); };
   float m = -__builtin_inff(), l = 0.0f;
   f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
   if constexpr (ONE) {
@@ -1046,7 +1093,7 @@ int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
   const bool sel = a.selected != nullptr;
   a.scanned = !sel && a.requests > SCAN_REQUESTS;
   if (a.scanned) {
-    hipLaunchKernelGGL(kv_scan_kernel, dim3(1), dim3(1024), 0, s, a, sh.tile_rows);
+    hipLaunchKernelGGL(kv_scan_kernel, dim3(1), dim3(1024), 0, s, a, sh.tile_rows, 0);
     KV_HIP_TRY(hipGetLastError());
   }
   const size_t lists = sel || a.scanned ? 0 : ((size_t)a.requests + 3 * (size_t)(a.requests + 1)) * 4;
@@ -1081,11 +1128,11 @@ int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
   const int64_t most = a.tokens * (int64_t)a.group;
   if (sh.tile_rows == 16) {
     const int rows = (int)(sel && a.group < 16 ? a.group : most < 16 ? most : 16);
-    hipLaunchKernelGGL((kv_join_kernel<D, DT, true>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a, 16);
+    hipLaunchKernelGGL((kv_join_kernel<D, DT, true>), dim3((unsigned)(a.n_wg - 1), (unsigned)rows), dim3(256), 0, s, a, 16, 0);
   } else {
     constexpr int SETS = 256 / (D / 4);
     hipLaunchKernelGGL((kv_join_kernel<D, DT, false>), dim3((unsigned)(a.n_wg - 1), (unsigned)((sh.tile_rows + SETS - 1) / SETS)),
-                       dim3(256), 0, s, a, sh.tile_rows);
+                       dim3(256), 0, s, a, sh.tile_rows, 0);
   }
   KV_HIP_TRY(hipGetLastError());
   return IVFPQ_OK;

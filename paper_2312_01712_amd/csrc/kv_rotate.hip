@@ -22,7 +22,7 @@ __device__ inline void turn_of(int32_t position, uint64_t phase, float &c, float
 }
 
 // A thread has 16 channels (8 pairs, or 16 that are not turned) of every slots-th head of a token, so that it computes its
-// sines once for them.  Bound by memory: 9001 tokens of 40 heads of 128, 184 MB, 41 us (4.5 TB/s); one of 24 heads 2.4 us.
+// sines once for them.  Bound by memory: 9001 tokens of 40 heads of 128, 184 MB, 37 us (5 TB/s); one of 24 heads 2.3 us.
 template <int D, int DT, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void kv_rotate_kernel(KvRotateArgs a) {
   constexpr int CHUNKS = D / 16;

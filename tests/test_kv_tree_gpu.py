@@ -229,6 +229,30 @@ def test_trees_in_wide_tables(kv, dtype, H, G, D, new, window):
     s.attend_tree(H * G)
 
 
+@pytest.mark.parametrize("D,G,new", [(128, 4, 16), (128, 1, 40), (96, 5, 13), (64, 16, 8), (256, 3, 20)])
+@pytest.mark.parametrize("window", [0, 2500])
+def test_one_tree_behind_a_long_context(kv, D, G, new, window):
+    """One request whose units of three, four and more tiles go into parts of a few pages, some of which end between the two
+    wavefronts that take a unit's pages in turn."""
+    rng = np.random.default_rng(D + G + window)
+    s = TreeServer(kv, rng, "bf16", 2, D, 160, 1, 30000)
+    s.fill([9001])
+    s.draft([new], window=window)
+    s.attend_tree(2 * G)
+
+
+@pytest.mark.parametrize("R,D,G", [(30, 128, 4), (31, 128, 4), (70, 128, 8), (70, 64, 3)])
+def test_trees_of_requests_whose_lists_fill_the_lds(kv, R, D, G):
+    """Lists of the requests beside the pages in LDS, and from a launch of their own where they do not fit there."""
+    rng = np.random.default_rng(R + D + G)
+    s = TreeServer(kv, rng, "fp16", 2, D, 8 * R, R, 6000)
+    s.fill(rng.integers(0, 400, R))
+    new = rng.integers(0, 18, R)
+    s.draft(new, max_tokens=int(new.sum()) + 3)
+    s.attend_tree(2 * G)
+    s.keep()
+
+
 @pytest.mark.parametrize("G,W", [(1, 4), (8, 4), (4, 100)])
 def test_trees_of_more_requests_than_are_scanned_in_a_workgroup(kv, G, W):
     rng = np.random.default_rng(25)
