@@ -3,7 +3,8 @@
 // The kernels of kv_attention_kernels.h with masks, and one of its own for trees of some tokens: two to four tiles of 16 rows for a kv
 // head are too many for the kernel of decoding, which unpacks a page for every tile, and too few for that of chunks, which unpacks
 // pages into LDS for many.  Here a wavefront has pages of its own, as in decoding, but every fragment that it unpacks feeds the
-// products of two tiles.  Pages come into LDS without passing registers, so that three wavefronts fit a SIMD.
+// products of two tiles, and two wavefronts read a page at the same time for two tiles each.  Pages come into LDS without passing
+// registers, so that three wavefronts fit a SIMD.
 
 #include "kv_attention_kernels.h"
 
@@ -287,10 +288,10 @@ __device__ inline void tiles_pages(const KvAttnArgs &a, const Unit &u, Walk &wal
 
 // Units of up to NT tiles, shared out among workgroups as in kv_rows16_kernel; a workgroup's wavefronts have two tiles each and take the
 // unit's pages in turn, two for each pair of tiles or four for the only one, and add up through LDS.  Bound by the issue of
-// instructions (vector units 73 % busy, matrix units 33 %): a page and two tiles are 390 instructions of the vector units, half
-// of them unpacking, and 64 products.  16 tokens of 32 heads behind 300 001, 79 GFLOP, 328 MB, 112 us and 9 of joining (16 rows a tile as in
+// instructions (vector units 64 % busy, matrix units 28 %): a page and two tiles are 390 instructions of the vector units, half
+// of them unpacking, and 64 products.  16 tokens of 32 heads behind 300 001, 79 GFLOP, 328 MB, 114 us and 9 of joining (16 rows a tile as in
 // decoding: 168 in all; units of two tiles, which read every page twice, 118 and 10); trees of up to 32 tokens, 64 heads, behind 24
-// contexts to 33 000, 117 GFLOP, 181 us (in the kernel of chunks 245, in units of two tiles 188).  Three tiles a wavefront with two
+// contexts to 33 000, 117 GFLOP, 184 us with joining (in the kernel of chunks 245, in units of two tiles 188).  Three tiles a wavefront with two
 // wavefronts a SIMD took 160 and 282 us, four, which leave a few values to memory in the loop, 169 and 328; eight wavefronts a
 // workgroup 75 us where four took 60 (one request of 100 000).  Scaled products of the 4-bit codes themselves would save unpacking keys, but sum to
 // 2^-17 of the sizes' sum only, and take no 16-bit queries.
@@ -451,8 +452,8 @@ int tiles_of(KvAttnArgs a, const TreeShape &sh, hipStream_t s) {
   if (a.whole || a.n_wg == 1) return IVFPQ_OK;
   const int64_t most = a.tokens * (int64_t)a.group;
   const int rows = (int)(most < sh.tile_rows ? most : sh.tile_rows);
-  // few units of dozens of parts each: a workgroup a row; many of two or three: a workgroup 256 / (D / 4) rows (800 units
-  // over 768 shares: 21 us and 7)
+  // few units of dozens of parts each: a workgroup a row of a unit (of a share, most of which leave no unit across their border:
+  // 14 us for 8 units of 64 rows, now 9); many of two or three: a workgroup 256 / (D / 4) rows (800 units over 768 shares: 21 us and 7)
   if (sh.n_wg >= 8 * sh.units) {
     hipLaunchKernelGGL((kv_join_kernel<D, DT, true>), dim3((unsigned)sh.units, (unsigned)rows), dim3(256), 0, s, a, sh.tile_rows, a.n_wg - 1);
   } else {
