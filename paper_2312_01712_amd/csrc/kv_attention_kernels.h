@@ -957,10 +957,10 @@ __device__ inline int border_at(const KvAttnArgs &a, int shares, int i, int tid)
   return uniform(found);
 }
 
-// Units that several workgroups share.  Workgroup (w, y) adds up the parts of ROWS rows of the unit that goes across
-// the border behind share w and began in it, with `shares` the w-th such unit of that many shares.  D / 4 lanes have a part (ROWS = 1) or a row each: decode has one
-// tile of few rows and up to all shares in a unit (520 001 tokens, 64 shares a unit: 40 us with a thread a row
-// and 8 channels, now 5), chunks have many rows of few parts (a workgroup a row there: 29 us for 256 shares).
+// Units that several workgroups share.  Workgroup (w, y) adds up the parts of one row (ONE) or some of the unit that goes across
+// the border behind share w and began in it; with `shares`, of the w-th such unit of that many shares.  D / 4 lanes have a part (ONE)
+// or a row each: decode has one tile of few rows and up to all shares in a unit (520 001 tokens, 64 shares a unit: 40 us with a
+// thread a row and 8 channels, now 5), chunks have many rows of few parts (a workgroup a row there: 29 us for 256 shares).
 template <int D, int DT, bool ONE>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a, int tile_rows, int shares) {
   constexpr int LANES = D / 4, SETS = 256 / LANES;  // 96 channels: 24 lanes, 10 sets, 16 threads idle
