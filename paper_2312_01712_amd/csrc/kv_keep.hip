@@ -128,7 +128,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 4
   // (where the table's width has cut the request its length does not say where its new tokens begin)
   const int past = kv < a.width * (int64_t)KV_PAGE ? max(kv - n, 0) : max(a.positions[t0], 0);
   const int kept = min(stays - past, n);
-  if (kept <= 0 || kept == n) return;  // all of them stay where they are
+  if (kept < 0 || kept == n) return;  // all of them stay where they are
+  // (none of them: only the box is made, of what was held; `end` is then that of a token which is not used)
+  const int end = max(kept, 1) - 1;
   char *pages = a.pages[blockIdx.z] + (int64_t)h * kv_head_bytes(D);
   const int64_t page_bytes = a.kv_heads * (int64_t)kv_head_bytes(D);
   const uint64_t n_slots = a.n_pages * KV_PAGE;
@@ -138,7 +140,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 4
   int64_t own_from = -1, own_to = -1;
   int own_page = -1, in_place = kept;  // the first of them that moves
   if constexpr (SMALL) {
-    const int row = a.rows[t0 + min(lane, kept - 1)] - t0;
+    const int row = a.rows[t0 + min(lane, end)] - t0;
     own_to = lane < n ? a.slots[t0 + lane] : -1;
     own_page = first_column + lane < end_column ? a.table[(int64_t)r * a.width + first_column + lane] : -1;
     own_from = __shfl(own_to, row & 63);
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 4
     if (moved) in_place = __builtin_ctzll(moved);
   } else {
     for (int b = 0; b < kept; b += 64) {
-      const uint64_t moved = __ballot(b + lane < kept && a.rows[t0 + min(b + lane, kept - 1)] - t0 != b + lane);
+      const uint64_t moved = __ballot(b + lane < kept && a.rows[t0 + min(b + lane, end)] - t0 != b + lane);
       if (moved) {
         in_place = b + __builtin_ctzll(moved);
         break;
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 96 ? 4
   auto load = [&](int i0) {
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const int i = min(i0 + j, kept - 1);
+      const int i = min(i0 + j, end);
       const int64_t from = source(i);
       to[j] = target(i);
       if (i0 + j >= kept || from == to[j]) to[j] = -1;  // (also where one of the two is nowhere)

@@ -344,7 +344,8 @@ class Kept:
 def keep(caches: Sequence["KvCache"], step: Step, tree: Tree, drafted: torch.Tensor, picked: torch.Tensor, free_pages: torch.Tensor,
          free_state: torch.Tensor, out: Optional[Kept] = None) -> Kept:
     """What stays of a step's drafted tokens (`ivfpq_kv_keep`): of every request its first new token and the longest path behind
-    it whose tokens are those that the model picked.  They move together in all caches (of one shape), the boxes of their
+    it whose tokens are those that the model picked.  (With masks of the caller's own: the deepest token that sees only tokens that agree, and
+    what it sees; none of a request's where there is no such token, as in a block that sees all of itself and is refused.)  They move together in all caches (of one shape), the boxes of their
     pages are made again, pages behind them go back to the ring.  tree: the step's, without a window; drafted, picked [T] int32: the
     tokens, and what the model picks behind each; free_state: `step.free_state`.  Once per step."""
     caches = list(caches)

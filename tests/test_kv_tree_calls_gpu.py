@@ -1,0 +1,47 @@
+"""Calls of decoding with drafted tokens that a caller may make beside the usual ones, on the GPU."""
+import numpy as np
+import pytest
+import torch
+
+import kv_tree_reference as tref
+from test_kv_gpu import dev, kv  # noqa: F401
+from test_kv_tree_gpu import TreeServer
+
+pytestmark = pytest.mark.gpu
+
+
+def own_masks(s, sees):
+    """The step's tree with masks [T][max_nodes] of the caller's own."""
+    s.sees = sees
+    s.tree = s.kv.Tree(dev(tref.words(sees), torch.int64), s.tree.positions, s.tree.max_nodes)
+
+
+@pytest.mark.parametrize("dtype,H,D", [("bf16", 2, 128), ("fp16", 5, 64), ("bf16", 1, 96), ("fp16", 2, 256)])
+@pytest.mark.parametrize("n", [3, 30, 64, 65, 200])
+def test_keep_of_blocks_of_which_nothing_stays(kv, dtype, H, D, n):
+    """Blocks whose tokens see each other: one that does not agree goes as a whole, the request's first token with it, and
+    the box of the page that it began in is that of what was held."""
+    rng = np.random.default_rng(n + D)
+    s = TreeServer(kv, rng, dtype, H, D, 60, 6, 8)
+    s.fill([0, 10, 64, 100, 63, 127])
+    held = s.cache.boxes.clone()
+    new = [n, n, n, n, n, max(n // 2, 1)]
+    T = s.draft(new)
+    sees = np.zeros((T, n), bool)
+    drafted, picked = np.arange(T) % 7, (np.arange(T) + 1) % 7
+    for r, (a, b) in enumerate(zip(s.want["q_start"], s.want["q_start"][1:])):
+        first = (b - a) // 2 if r == 3 else b - a        # the fourth request has two blocks, of which the first agrees
+        sees[a:a + first, :first] = True
+        sees[a + first:b, :b - a] = True
+        if r < 4 and b - a > 1:
+            picked[b - 2] = -1
+    own_masks(s, sees)
+    kept = s.keep(drafted=drafted, picked=picked)
+    assert s.past.tolist() == [0, 10, 64, 100 + n // 2, 63 + n, 127 + max(n // 2, 1)] and (kept[:3 * n] == -1).all()
+    for r, column in ((1, 0), (2, 0)):
+        page = s.table[r, column]
+        assert torch.equal(s.cache.boxes[page].view(torch.int16), held[page].view(torch.int16))
+    # and on from there
+    s.draft([5, 40, 1, 9, 0, 70])
+    s.attend_tree(2 * H)
+    s.keep(agree=1.0)
