@@ -216,8 +216,9 @@ int ivfpq_kv_tree_attention(const ivfpq_kv_cache *cache, const ivfpq_kv_step *st
 /* What stays of a step's drafted tokens.  A request's first new token agrees; another that is stored agrees if drafted[it] ==
  * picked[its parent] (its parent: the last token before it that its mask names).  The deepest token whose mask names only tokens that
  * agree, the first among equals, and what it sees stay, in this order, behind what was held; the request's other new tokens are
- * held no more.  A first token that sees only itself, as in a tree, stays in any case; with other masks there may be no such token, and
- * then none of the request's stays (a first token that has seen refused ones among them).  tree: one without a window.
+ * held no more.  Bits of tokens that are not there are not looked at.  A first token that sees only itself, as in a tree, stays in
+ * any case; with other masks there may be no such token, and then none of the request's stays (a first token that has seen refused
+ * ones among them).  tree: one without a window.
  *   drafted, picked  device [max_tokens] int32: the tokens, and those that the model picks behind each
  *   lens    device [requests]: tokens held from now on, past_lens of the next step
  *   rows    device [max_tokens]: from q_start[r] on the rows that stay of request r, -1 behind them

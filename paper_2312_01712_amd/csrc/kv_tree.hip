@@ -95,6 +95,10 @@ __global__ __launch_bounds__(THREADS) void kv_accept_kernel(KvKeepArgs a) {
     const Fresh f = fresh_of(a.q_start, r, a.tokens);
     const int n = min(f.n, a.max_nodes), words = a.words, kv = a.kv_lens[r];
     const uint64_t *mask = a.masks + (int64_t)(f.t0 + i) * words;
+    auto named = [&](int w) -> uint64_t {  // without bits of tokens that are not there
+      const int there = n - w * 64;
+      return mask[w] & (there >= 64 ? ~0ull : there > 0 ? (1ull << there) - 1 : 0);
+    };
     bool agrees = false;
     if (i < n) {
       const int64_t slot = a.slots[f.t0 + i];
@@ -118,7 +122,7 @@ __global__ __launch_bounds__(THREADS) void kv_accept_kernel(KvKeepArgs a) {
       bool good = true;
       int depth = 0;
       for (int w = 0; w < words; ++w) {
-        const uint64_t x = mask[w];
+        const uint64_t x = named(w);
         good = good && (x & ~agree[w]) == 0;
         depth += __builtin_popcountll(x);
       }
@@ -130,7 +134,7 @@ __global__ __launch_bounds__(THREADS) void kv_accept_kernel(KvKeepArgs a) {
     __syncthreads();
     for (int w = 0; w < THREADS / 64; ++w) top = max(top, best[w]);
     if (rank >= 0 && rank == top)
-      for (int w = 0; w < words; ++w) path[w] = mask[w];
+      for (int w = 0; w < words; ++w) path[w] = named(w);
     __syncthreads();
     int kept = 0, before = 0;
     for (int w = 0; w < words; ++w) {

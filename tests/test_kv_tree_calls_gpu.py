@@ -45,3 +45,20 @@ def test_keep_of_blocks_of_which_nothing_stays(kv, dtype, H, D, n):
     s.draft([5, 40, 1, 9, 0, 70])
     s.attend_tree(2 * H)
     s.keep(agree=1.0)
+
+
+@pytest.mark.parametrize("n", [20, 64, 90])
+@pytest.mark.parametrize("density", [0.02, 0.3])
+def test_keep_with_any_masks(kv, n, density):
+    """Paths from anywhere: without the first token, with later ones, tokens that see nothing, bits of tokens that are not there."""
+    rng = np.random.default_rng(n)
+    s = TreeServer(kv, rng, "bf16", 3, 64, 90, 12, 8)
+    s.fill(rng.integers(0, 140, 12))
+    for step in range(3):
+        new = rng.integers(1, n + 1, 12)
+        T = s.draft(new, max_nodes=n)
+        sees = rng.random((T, n)) < density
+        sees[:, 0] |= rng.random(T) < 0.3
+        sees[::7] = False
+        own_masks(s, sees)
+        s.keep(drafted=rng.integers(0, 2, T) * (step < 2), picked=rng.integers(0, 2, T) * (step < 2))
