@@ -4,8 +4,8 @@ import pytest
 import torch
 
 import kv_tree_reference as tref
-from test_kv_gpu import dev, kv  # noqa: F401
-from test_kv_tree_gpu import TreeServer
+from test_kv_gpu import TYPES, dev, kv  # noqa: F401
+from test_kv_tree_gpu import TreeServer, random_parents
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +62,43 @@ def test_keep_with_any_masks(kv, n, density):
         sees[::7] = False
         own_masks(s, sees)
         s.keep(drafted=rng.integers(0, 2, T) * (step < 2), picked=rng.integers(0, 2, T) * (step < 2))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("new", [[4] * 12, [9, 1, 30, 0, 17, 2, 5, 8, 8, 8, 1, 3], [70, 3, 40] + [1] * 9])
+def test_trees_made_without_a_word_on_their_size(kv, dtype, new):
+    """max_nodes left out: as many as the step has rows, whatever its requests have."""
+    rng = np.random.default_rng(sum(new))
+    s = TreeServer(kv, rng, dtype, 2, 128, 140, 12, 70)
+    s.fill(rng.integers(0, 600, 12))
+    T = s.draft(new)
+    small = s.tree
+    s.tree = kv.tree(dev(s.parents, torch.int32), s.step)
+    assert s.tree.max_nodes == T and torch.equal(s.tree.positions, small.positions)
+    s.sees, _ = tref.tree(s.parents, s.want, T)
+    assert np.array_equal(s.tree.masks.cpu().numpy(), tref.words(s.sees))
+    s.attend_tree(8)
+    s.keep(agree=0.8)
+
+
+def test_boxes_of_zeros_of_both_signs(kv):
+    """The box after `keep` has the zeros of either sign that appending only the kept gives."""
+    rng = np.random.default_rng(5)
+
+    def edit(k, v):
+        k.copy_(dev(np.where(rng.random(tuple(k.shape)) < 0.5, -0.0, 0.0), TYPES["bf16"]))
+    s = TreeServer(kv, rng, "bf16", 2, 64, 30, 4, 5)
+    s.fill([0, 1, 64, 66], edit=edit)
+    other = kv.KvCache(30, 2, 64)
+    other.pages.copy_(s.cache.pages), other.boxes.copy_(s.cache.boxes)
+    new = np.array([7, 9, 12, 5])
+    s.draft(new, parents=random_parents(rng, new), edit=edit)
+    k, v = s.cache.read(s.step.slots)
+    kept = s.keep(agree=1.0)
+    start, slots = s.want["q_start"], s.step.slots
+    to = [start[r] + i for r in range(4) for i in range(s.past[r] - s.before[r])]
+    stay = dev(kept[to], torch.int64)
+    other.append(k[stay].contiguous(), v[stay].contiguous(), slots[dev(np.array(to), torch.int64)].contiguous())
+    pages = np.unique([s.table[r, j // 64] for r in range(4) for j in range(s.past[r])])
+    a, b = (c.boxes[dev(pages, torch.int64)].view(torch.int16) for c in (s.cache, other))
+    assert torch.equal(a, b) and (a == 0).any() and (a != 0).any()
