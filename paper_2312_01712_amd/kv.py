@@ -253,14 +253,14 @@ def _fits(step: Step, tree: Tree) -> None:
         raise ValueError(f"tree: {tree.max_tokens} rows on cuda:{tree._checked}, the step has {step.max_tokens} on cuda:{step._checked}")
 
 
-def tree(parents: torch.Tensor, step: Step, max_nodes: Optional[int] = None, window: int = 0, out: Optional[Tree] = None) -> Tree:
+def tree(parents: torch.Tensor, step: Step, max_nodes: Optional[int] = None, window: Optional[int] = None, out: Optional[Tree] = None) -> Tree:
     """What drafted tokens see of each other, and their positions (`ivfpq_kv_tree_plan`).  parents [T] int32: the number, within
     its request, of the token that each hangs on; -1: none.  max_nodes: no request has more new tokens (T unless given, 1024 at
-    most); window: positions that a token sees, its own among them (0: all)."""
+    most); window: positions that a token sees, its own among them (0: all).  Both are those of `out` where that is given."""
     if out is None:
-        out = Tree.empty(step.max_tokens, min(max(step.max_tokens, 1), MAX_NODES) if max_nodes is None else max_nodes, window,
+        out = Tree.empty(step.max_tokens, min(max(step.max_tokens, 1), MAX_NODES) if max_nodes is None else max_nodes, window or 0,
                          step.table.device)
-    elif (max_nodes is not None and max_nodes != out.max_nodes) or (window and window != out.window):
+    elif (max_nodes is not None and max_nodes != out.max_nodes) or (window is not None and window != out.window):
         raise ValueError(f"tree: out was made for max_nodes = {out.max_nodes} and window = {out.window}")
     _fits(step, out)
     dev = step._checked

@@ -102,3 +102,20 @@ def test_boxes_of_zeros_of_both_signs(kv):
     pages = np.unique([s.table[r, j // 64] for r in range(4) for j in range(s.past[r])])
     a, b = (c.boxes[dev(pages, torch.int64)].view(torch.int16) for c in (s.cache, other))
     assert torch.equal(a, b) and (a == 0).any() and (a != 0).any()
+
+
+def test_trees_into_buffers_with_a_window(kv):
+    """Nothing said: the window of `out`; the same said; none, or another, refused."""
+    rng = np.random.default_rng(6)
+    s = TreeServer(kv, rng, "bf16", 1, 64, 8, 2, 4)
+    s.fill([20, 30])
+    s.draft([9, 14], window=3)
+    parents = dev(s.parents, torch.int32)
+    for window in (None, 3):
+        out = kv.Tree.empty(len(s.parents), 14, 3)
+        assert kv.tree(parents, s.step, window=window, out=out) is out
+        assert torch.equal(out.masks, s.tree.masks) and torch.equal(out.positions, s.tree.positions)
+    for window in (0, 2):
+        with pytest.raises(ValueError):
+            kv.tree(parents, s.step, window=window, out=out)
+    assert kv.tree(parents, s.step, max_nodes=14).window == 0
