@@ -146,6 +146,12 @@ def _int32(x: int, what: str) -> int:
     return x
 
 
+def _needs_gradient() -> None:
+    """For inputs whose gradient a result without a graph would lose."""
+    if torch.is_grad_enabled():
+        raise ValueError("there is no backward pass: inputs that need a gradient are taken under torch.no_grad() or detached")
+
+
 def _heads_of(q: torch.Tensor) -> int:
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q: expected a tensor [tokens][heads][head_dim]")
@@ -297,8 +303,10 @@ class Rotary:
                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """q [T][heads][head_dim] and k [T][kv_heads][head_dim] turned by positions [axes][T] int32 ([T]: the same on every axis);
         a token whose first position is negative is left out: its rows are not written.  out: two tensors for the results, q and k
-        themselves among them; no other overlap."""
+        themselves among them; no other overlap.  There is no backward pass: q and k that need a gradient are refused."""
         heads, kv_heads, dev = _heads_of(q), _heads_of(k), self.device
+        if q.requires_grad or k.requires_grad:
+            _needs_gradient()
         T, _, D = q.shape
         dtype = q.dtype
         if dtype not in _DTYPES:
@@ -446,7 +454,7 @@ class KvCache:
         them (0: all); pages: [T][kv_heads][n] int32 as from `select`, in any order, none twice (its tokens would count
         twice); max_new: no request has more new tokens (T unless given).  It decides how the work is cut and not what is
         computed: without it a batch that decodes goes through the kernel of chunks, which takes longer.  Returns
-        (out as q, rows that do not overlap; lse [T][heads] fp32)."""
+        (out as q, rows that do not overlap; lse [T][heads] fp32), without a graph: there is no backward pass."""
         T, heads, dev, dtype = step.max_tokens, _heads_of(q), self.device, self.dtype
         shape = (T, heads, self.head_dim)
         qr = _rows(q, dtype, shape, dev, "q")
@@ -483,8 +491,11 @@ class KvCache:
                        lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
         """Drafted tokens' attention over the cache (`ivfpq_kv_tree_attention`): over what their requests held before the step (with a
         window of the tree the last of it) and over the new tokens that their masks name.  q [T][heads][head_dim]; scale: head_dim
-        ** -0.5 unless given.  Returns (out as q, rows that do not overlap; lse [T][heads] fp32)."""
+        ** -0.5 unless given.  There is no backward pass: a q that needs a gradient is refused.  Returns (out as q, rows that do not
+        overlap; lse [T][heads] fp32)."""
         T, heads, dev, dtype = step.max_tokens, _heads_of(q), self.device, self.dtype
+        if q.requires_grad:
+            _needs_gradient()
         _fits(step, tree)
         shape = (T, heads, self.head_dim)
         qr = _rows(q, dtype, shape, dev, "q")

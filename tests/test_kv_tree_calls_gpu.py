@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import kv_tree_reference as tref
-from test_kv_gpu import TYPES, dev, kv  # noqa: F401
+from test_kv_gpu import TYPES, dev, kv, rows  # noqa: F401
 from test_kv_tree_gpu import TreeServer, random_parents
 
 pytestmark = pytest.mark.gpu
@@ -119,3 +119,24 @@ def test_trees_into_buffers_with_a_window(kv):
         with pytest.raises(ValueError):
             kv.tree(parents, s.step, window=window, out=out)
     assert kv.tree(parents, s.step, max_nodes=14).window == 0
+
+
+def test_projections_with_weights_that_need_gradients(kv):
+    """Under no_grad, in place in the rows of a projection, the results are those of detached tensors; outside they are refused."""
+    rng = np.random.default_rng(7)
+    s = TreeServer(kv, rng, "bf16", 2, 64, 8, 2, 4)
+    s.fill([20, 30])
+    T = s.draft([9, 14])
+    x, weight = rows(rng, "bf16", T, 32)[0], rows(rng, "bf16", 32, 6 * 64, spread=0.2)[0].requires_grad_()
+    rotary = kv.Rotary([10000.0 ** (-i / 32) for i in range(32)])
+    made = (x @ weight).unflatten(-1, (6, 64))
+    with pytest.raises(ValueError, match="gradient"):
+        rotary(made[:, :4], made[:, 4:], s.tree.positions)
+    with pytest.raises(ValueError, match="gradient"):
+        s.cache.tree_attention(made[:, :4], s.step, s.tree)
+    want = rotary(made[:, :4].detach(), made[:, 4:].detach(), s.tree.positions)
+    with torch.no_grad():
+        made = (x @ weight).unflatten(-1, (6, 64))
+        got = rotary(made[:, :4], made[:, 4:], s.tree.positions, out=(made[:, :4], made[:, 4:]))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert torch.equal(s.cache.tree_attention(got[0], s.step, s.tree)[0], s.cache.tree_attention(want[0], s.step, s.tree)[0])
