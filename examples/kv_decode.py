@@ -65,7 +65,7 @@ class Server:
         q, k, v = layer.project(x)
         step = kv.plan(self.lens, torch.tensor(new, dtype=torch.int32, device="cuda"), self.table, self.free_pages,
                        self.free_state, max_tokens=x.shape[0])
-        tree = kv.tree(parents, step, max_nodes=max(new))
+        tree = kv.tree(parents, step, max_nodes=max(max(new), 1))
         q, k = self.rotary(q, k, tree.positions, out=(q, k))
         cache.append(k, v, step.slots)
         out, _ = cache.tree_attention(q, step, tree)

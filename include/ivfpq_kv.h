@@ -170,7 +170,7 @@ typedef struct {
 
 /* Rotary positions.  Pair i of a row's first `turned` channels, channels i and i + turned / 2 or (neighbours) 2 i and 2 i + 1, is
  * turned by the angle positions[axis[i]] * f_i:  (a, b) -> (a cos - b sin, b cos + a sin).  Frequencies are given in turns, as 64-bit
- * fractions of one: phases[i] = round(f_i / (2 pi) * 2^64) modulo 2^64, so that far positions lose nothing. */
+ * fractions of one: phases[i] = round(f_i / (2 pi) * 2^64) modulo 2^64, so that the angle at position p is |p| * 2^-65 turns off at most. */
 #define IVFPQ_KV_MAX_AXES 8
 typedef struct {
   int32_t head_dim;       /* 64, 96, 128 or 256                                                  */
@@ -193,7 +193,8 @@ int ivfpq_kv_rotate(const ivfpq_kv_rotary *rotary, ivfpq_kv_rows q, int32_t head
  * request's new ones, or none; it sees itself, its parent, that one's parent and so on. */
 #define IVFPQ_KV_MAX_NODES 1024
 typedef struct {
-  int32_t max_nodes;   /* no request has more new tokens, 1 .. IVFPQ_KV_MAX_NODES; tokens beyond it see none of the new ones */
+  int32_t max_nodes;   /* no request has more new tokens, 1 .. IVFPQ_KV_MAX_NODES; tokens beyond it see none of the new ones.
+                          It is the masks' width, and ivfpq_kv_tree_attention chooses its kernel by it: give the largest tree's */
   int32_t window;      /* 0: none; otherwise a token sees itself and the window - 1 positions before it */
   uint64_t *masks;     /* device [max_tokens][(max_nodes + 63) / 64]: bit j % 64 of word j / 64: token j is seen */
   int32_t *positions;  /* device [max_tokens]: position of the request's first new token, plus the ancestors' number; -1: no token */

@@ -1,4 +1,5 @@
-// Attention of a step's new tokens over the paged 4-bit cache, all pages or selected ones.
+// Attention of a step's new tokens over the paged 4-bit cache, all pages or selected ones, or with masks: what the units that launch
+// it share (kv_attention.hip, kv_tree_attention.hip).
 //
 // The running form of the softmax: with s_j = scale log2(e) q . k_j, a row keeps m = max s_j (or a number near it),
 // l = sum 2^(s_j - m) and o = sum 2^(s_j - m) v_j and multiplies l and o by 2^(m_old - m_new) when m
@@ -11,8 +12,8 @@
 // product are, in place, the second operand of the second: lane (g, row) has keys 16 tt + 4 g + i, and
 // the page stores the values in this order of tokens.
 //
-// Two kernels.  kv_rows16_kernel: 16 rows or fewer share a page (decode, selected pages); its wavefronts have
-// pages of their own, held in registers from memory to the products.  kv_rows_kernel: many rows share a
+// Two kernels here; trees have a third (kv_tree_attention.hip).  kv_rows16_kernel: 16 rows or fewer share a page (decode, selected
+// pages); its wavefronts have pages of their own, held in registers from memory to the products.  kv_rows_kernel: many rows share a
 // page (chunks of prompts); a workgroup unpacks a page into LDS once and its wavefronts have 32 rows each.
 
 #pragma once
@@ -26,7 +27,7 @@ namespace ivfpq {
 namespace {
 
 constexpr int SCAN_REQUESTS = 512;  // more than these: their units are scanned by a launch of its own
-constexpr int UNIT_EXTRA = 8;       // see unit_extra
+constexpr int UNIT_EXTRA = 8;       // pages that a unit in tiles counts beside its own: see unit_weight
 constexpr int WHOLE_PAGES = 32;     // tables up to this width: a workgroup has whole units, nothing is joined
 
 // over the four lanes that hold a row: lanes 16 apart
@@ -268,12 +269,10 @@ struct Requests {
 __device__ inline int unit_weight(int rows) { return rows > 32 ? 2 : 1; }
 
 struct TileUnits {
-  int64_t rows;
   int tiles, full, last, head;  // units of a head, indexes of a unit of 64 rows, of the last one, of a head
 };
 __device__ inline TileUnits tile_units(int64_t rows, int pages, bool whole) {
   TileUnits t;
-  t.rows = rows;
   t.tiles = (int)((rows + 63) / 64);
   t.full = whole ? 1 : 2 * (pages + UNIT_EXTRA);
   t.last = whole ? 1 : unit_weight((int)(rows - 64 * (int64_t)(t.tiles - 1))) * (pages + UNIT_EXTRA);
@@ -1100,13 +1099,15 @@ int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
   int rc;
   if (sh.tile_rows == 16) {
     const size_t lds = (size_t)(4 * 16 * (D + 4) + 4 * 16 * 2) * 4 + 4 * 4 + lists;
-    if (!TREE && sel) {
-      if ((rc = allow_lds(&kv_rows16_kernel<D, DT, true>, lds))) return rc;
-      hipLaunchKernelGGL((kv_rows16_kernel<D, DT, true>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
-    } else {
-      if ((rc = allow_lds(&kv_rows16_kernel<D, DT, false, TREE>, lds))) return rc;
-      hipLaunchKernelGGL((kv_rows16_kernel<D, DT, false, TREE>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
-    }
+    auto rows16 = [&](auto SEL) -> int {
+      constexpr bool select = decltype(SEL)::value;
+      if ((rc = allow_lds(&kv_rows16_kernel<D, DT, select, TREE>, lds))) return rc;
+      hipLaunchKernelGGL((kv_rows16_kernel<D, DT, select, TREE>), dim3((unsigned)a.n_wg), dim3(256), lds, s, a);
+      return IVFPQ_OK;
+    };
+    if constexpr (TREE) rc = rows16(std::false_type());  // (a tree's tokens have no selected pages)
+    else rc = sel ? rows16(std::true_type()) : rows16(std::false_type());
+    if (rc) return rc;
   } else {
     const size_t lds = (size_t)2 * page_fragments<D>() * 1024 + 8 * 4 + lists;
     if constexpr (D == 256) {
@@ -1138,11 +1139,6 @@ int attention_of(KvAttnArgs a, const Shape &sh, hipStream_t s) {
   return IVFPQ_OK;
 }
 
-template <int D, bool TREE>
-int attention_typed(const KvAttnArgs &a, int dtype, const Shape &sh, hipStream_t s) {
-  return dtype == IVFPQ_KV_BF16 ? attention_of<D, IVFPQ_KV_BF16, TREE>(a, sh, s) : attention_of<D, IVFPQ_KV_FP16, TREE>(a, sh, s);
-}
-
 void place_workspace(KvAttnArgs &a, const Shape &sh, char *workspace) {
   a.n_wg = sh.n_wg;
   a.whole = sh.whole;
@@ -1150,23 +1146,6 @@ void place_workspace(KvAttnArgs &a, const Shape &sh, char *workspace) {
   a.borders = reinterpret_cast<int32_t *>(workspace + sh.prefix);
   a.part_ml = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders);
   a.part_o = reinterpret_cast<float *>(workspace + sh.prefix + sh.borders + sh.ml);
-}
-
-template <bool TREE>
-int launch_attention(KvAttnArgs a, int D, int dtype, int max_new, char *workspace, hipStream_t s) {
-  const Shape sh = shape_of(a.tokens, a.requests, a.kv_heads, a.group, D, max_new, a.window, a.selected ? a.n_select : 0,
-                            a.width);
-  if (!launch_fits(sh.n_wg, sh.tile_rows == 256 || (sh.tile_rows == 128 && D == 256) ? 512 : 256)) {
-    set_error("kv_attention: %d workgroups are too many for one launch", sh.n_wg);
-    return IVFPQ_ERR_UNSUPPORTED;
-  }
-  place_workspace(a, sh, workspace);
-  switch (D) {
-    case 64: return attention_typed<64, TREE>(a, dtype, sh, s);
-    case 96: return attention_typed<96, TREE>(a, dtype, sh, s);
-    case 128: return attention_typed<128, TREE>(a, dtype, sh, s);
-    default: return attention_typed<256, TREE>(a, dtype, sh, s);
-  }
 }
 
 }  // namespace

@@ -80,7 +80,7 @@ struct KvRotateArgs {
   const int32_t *positions, *axis;
   const uint64_t *phases;
   int64_t q_token, q_head, k_token, k_head, qo_token, qo_head, ko_token, ko_head, axis_stride, tokens;
-  int32_t heads, kv_heads, axes, turned, dim, per, slots;  // per: heads of a thread; slots: threads that share a token's heads
+  int32_t heads, kv_heads, axes, turned, dim, slots;  // slots: threads that share a token's heads
 };
 
 struct KvTreeArgs {

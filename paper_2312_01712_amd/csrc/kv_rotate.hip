@@ -1,9 +1,10 @@
 // Rotary positions: pairs of channels of queries and keys turned by an angle, frequency times position, where every pair
 // has its own frequency and its own axis of the position.
 //
-// Angles are counted in turns, as 64-bit fractions of one: frequency / 2 pi times 2^64, times a whole position, modulo 2^64, is
-// the exact fraction of a turn whatever the position (in 32 bits a position of 10^6 would leave an angle 0.06 off).  Its
-// upper 32 bits go to the hardware's sine and cosine, which take turns (2^-22.9 off at most, over 2^20 turns from -1/2 to 1/2).
+// Angles are counted in turns, as 64-bit fractions of one: frequency / 2 pi times 2^64, rounded once, times a whole position p, modulo
+// 2^64, is off by |p| 2^-65 turns at most (2^-34 at the farthest; in 32 bits a position of 10^6 would leave an angle 0.06 off).  What
+// goes to the hardware's sine and cosine, which take turns, is its upper 32 bits (2^-32) as a 32-bit float from -1/2 to 1/2 (2^-26
+// turns, 2^-23.3 of an angle, at most).  Sine and cosine themselves were 2^-22.9 off at most of 2^20 places; no bound is documented.
 
 #include "kv_internal.h"
 

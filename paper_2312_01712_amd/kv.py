@@ -262,7 +262,8 @@ def _fits(step: Step, tree: Tree) -> None:
 def tree(parents: torch.Tensor, step: Step, max_nodes: Optional[int] = None, window: Optional[int] = None, out: Optional[Tree] = None) -> Tree:
     """What drafted tokens see of each other, and their positions (`ivfpq_kv_tree_plan`).  parents [T] int32: the number, within
     its request, of the token that each hangs on; -1: none.  max_nodes: no request has more new tokens (T unless given, 1024 at
-    most); window: positions that a token sees, its own among them (0: all).  Both are those of `out` where that is given."""
+    most).  It decides how wide masks are and how `tree_attention` cuts its work, not what is computed: with several requests give the
+    largest tree's, as T takes many small trees for a few large ones, which is slower.  window: positions that a token sees, its own among them (0: all).  Both are those of `out` where that is given."""
     if out is None:
         out = Tree.empty(step.max_tokens, min(max(step.max_tokens, 1), MAX_NODES) if max_nodes is None else max_nodes, window or 0,
                          step.table.device)
@@ -281,7 +282,8 @@ _TWO_PI = 10096689509235987743946820282484873672429286842977325943070736
 class Rotary:
     """Rotary positions (`ivfpq_kv_rotate`).  frequencies: radians a position, one for each pair of channels (their number a
     multiple of 8: the first 2 len(frequencies) channels are turned); axes: which axis of the position turns each pair (all the first,
-    unless given), such as time, height and width; neighbours: pairs are channels 2 i and 2 i + 1 instead of i and i + len(frequencies)."""
+    unless given), such as time, height and width; neighbours: pairs are channels 2 i and 2 i + 1 instead of i and i + len(frequencies).
+    To be made once for a model: its table is computed on the host in whole numbers (half a millisecond) and depends on no position."""
 
     def __init__(self, frequencies: Sequence[float], axes: Optional[Sequence[int]] = None, neighbours: bool = False, device=None):
         frequencies = [float(f) for f in frequencies]
