@@ -140,3 +140,17 @@ def test_projections_with_weights_that_need_gradients(kv):
         got = rotary(made[:, :4], made[:, 4:], s.tree.positions, out=(made[:, :4], made[:, 4:]))
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         assert torch.equal(s.cache.tree_attention(got[0], s.step, s.tree)[0], s.cache.tree_attention(want[0], s.step, s.tree)[0])
+
+
+def test_the_example_checks_a_step_without_drafts(kv):
+    """Server.check of examples/kv_decode.py where no request has new tokens: nothing changes."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import kv_decode
+    server = kv_decode.Server(kv_decode.Layer(64, heads=2, kv_heads=1, head_dim=64), 2, 128, n_pages=4)
+    x = torch.randn(5, 64, device="cuda").bfloat16()
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    server.step(x, [2, 3])
+    y, kept = server.check(x[:0], none, [0, 0], none, lambda y: none)
+    assert y.shape == (0, 64) and kept.rows.numel() == 0 and server.lens.tolist() == [2, 3] and int(server.free_state[2]) == 0
