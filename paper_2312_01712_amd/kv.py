@@ -147,9 +147,9 @@ def _int32(x: int, what: str) -> int:
 
 
 def _needs_gradient() -> None:
-    """For inputs whose gradient a result without a graph would lose."""
+    """For tensors whose gradient a result without a graph would lose, or that a graph holds and a result would overwrite."""
     if torch.is_grad_enabled():
-        raise ValueError("there is no backward pass: inputs that need a gradient are taken under torch.no_grad() or detached")
+        raise ValueError("there is no backward pass: tensors that need a gradient are taken under torch.no_grad() or detached")
 
 
 def _heads_of(q: torch.Tensor) -> int:
@@ -305,7 +305,7 @@ class Rotary:
                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """q [T][heads][head_dim] and k [T][kv_heads][head_dim] turned by positions [axes][T] int32 ([T]: the same on every axis);
         a token whose first position is negative is left out: its rows are not written.  out: two tensors for the results, q and k
-        themselves among them; no other overlap.  There is no backward pass: q and k that need a gradient are refused."""
+        themselves among them; no other overlap.  There is no backward pass: tensors that need a gradient are refused."""
         heads, kv_heads, dev = _heads_of(q), _heads_of(k), self.device
         if q.requires_grad or k.requires_grad:
             _needs_gradient()
@@ -320,6 +320,8 @@ class Rotary:
         if out is None:
             out = torch.empty(shape_q, dtype=dtype, device=q.device), torch.empty(shape_k, dtype=dtype, device=q.device)
         to_q, to_k = _rows(out[0], dtype, shape_q, dev, "out q"), _rows(out[1], dtype, shape_k, dev, "out k")
+        if out[0].requires_grad or out[1].requires_grad:
+            _needs_gradient()
         ref = self._refs.get((D, dtype))
         if ref is None:
             c = _Rotary(_int32(D, "head_dim"), self.turned, self.neighbours, _DTYPES[dtype], self.axes, self._phases.data_ptr(), self._axis.data_ptr())
@@ -493,7 +495,7 @@ class KvCache:
                        lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
         """Drafted tokens' attention over the cache (`ivfpq_kv_tree_attention`): over what their requests held before the step (with a
         window of the tree the last of it) and over the new tokens that their masks name.  q [T][heads][head_dim]; scale: head_dim
-        ** -0.5 unless given.  There is no backward pass: a q that needs a gradient is refused.  Returns (out as q, rows that do not
+        ** -0.5 unless given.  There is no backward pass: tensors that need a gradient are refused.  Returns (out as q, rows that do not
         overlap; lse [T][heads] fp32)."""
         T, heads, dev, dtype = step.max_tokens, _heads_of(q), self.device, self.dtype
         if q.requires_grad:
@@ -507,6 +509,8 @@ class KvCache:
         if lse is None:
             lse = torch.empty((T, heads), dtype=torch.float32, device=q.device)
         to_lse = _ptr(lse, torch.float32, (T, heads), dev, "lse")
+        if out.requires_grad or lse.requires_grad:
+            _needs_gradient()
         ws = self.tree_attention_workspace(step, heads, tree) if workspace is None else workspace
         size = ws.shape[0]
         args = _Attention(qr, heads, 1, self.head_dim ** -0.5 if scale is None else scale, 0, None, 0, to.data, to.token_stride,

@@ -134,7 +134,16 @@ def test_projections_with_weights_that_need_gradients(kv):
         rotary(made[:, :4], made[:, 4:], s.tree.positions)
     with pytest.raises(ValueError, match="gradient"):
         s.cache.tree_attention(made[:, :4], s.step, s.tree)
-    want = rotary(made[:, :4].detach(), made[:, 4:].detach(), s.tree.positions)
+    q, k = made[:, :4].detach(), made[:, 4:].detach()
+    want = rotary(q, k, s.tree.positions)
+    lse = torch.zeros(T, 4, device="cuda")
+    held = made.detach().clone()
+    for call in (lambda: rotary(q, k, s.tree.positions, out=(made[:, :4], k.clone())), lambda: rotary(q, k, s.tree.positions, out=(q.clone(), made[:, 4:])),
+                 lambda: s.cache.tree_attention(q, s.step, s.tree, out=made[:, :4]),
+                 lambda: s.cache.tree_attention(q, s.step, s.tree, lse=lse.requires_grad_())):
+        with pytest.raises(ValueError, match="gradient"):      # nor are results written into what a graph holds
+            call()
+    assert torch.equal(made, held)
     with torch.no_grad():
         made = (x @ weight).unflatten(-1, (6, 64))
         got = rotary(made[:, :4], made[:, 4:], s.tree.positions, out=(made[:, :4], made[:, 4:]))
