@@ -170,7 +170,7 @@ typedef struct {
 
 /* Rotary positions.  Pair i of a row's first `turned` channels, channels i and i + turned / 2 or (neighbours) 2 i and 2 i + 1, is
  * turned by the angle positions[axis[i]] * f_i:  (a, b) -> (a cos - b sin, b cos + a sin).  Frequencies are given in turns, as 64-bit
- * fractions of one: phases[i] = round(f_i / (2 pi) * 2^64) modulo 2^64, so that the angle at position p is |p| * 2^-65 turns off at most. */
+ * fractions of one: phases[i] = round(f_i / (2 pi) * 2^64) modulo 2^64, so that rounding them costs |p| 2^-65 turns at position p. */
 #define IVFPQ_KV_MAX_AXES 8
 typedef struct {
   int32_t head_dim;       /* 64, 96, 128 or 256                                                  */

@@ -407,7 +407,8 @@ TreeShape tree_shape(int64_t tokens, int64_t requests, int kv_heads, int group, 
   // here 19, of 8000 34 and 35).  Otherwise this one up to 96 rows (32: 16 of 16 000 97 and 79; 64: the same 169 and 118, 16 of 8000 92 and
   // 72; 96: 32 of 4000 110 and 89), the kernels of chunks beyond (128: 32 of 1500 50 and 64, of 4000 119 and 121; 256: 157 and 209), but where
   // requests have fewer tokens than the largest, whose tiles they leave part empty (64 of up to 8000, trees of up to 128 rows 147
-  // and 101, 512 365 and 286).
+  // and 101, 512 365 and 286).  `work` counts the table's width, as the host does not know what requests hold; each of its borders
+  // rests on two or three shapes, which differ by little there.
   const int64_t work = ((tokens * group + 15) / 16 + requests) * kv_heads * most;
   const bool ragged = tokens * 8 <= requests * nodes * 7 && rows <= 512;
   if (rows <= 64) s.tiles = rows > 16 && work >= 49152;

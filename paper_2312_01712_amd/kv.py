@@ -263,7 +263,8 @@ def tree(parents: torch.Tensor, step: Step, max_nodes: Optional[int] = None, win
     """What drafted tokens see of each other, and their positions (`ivfpq_kv_tree_plan`).  parents [T] int32: the number, within
     its request, of the token that each hangs on; -1: none.  max_nodes: no request has more new tokens (T unless given, 1024 at
     most).  It decides how wide masks are and how `tree_attention` cuts its work, not what is computed: with several requests give the
-    largest tree's, as T takes many small trees for a few large ones, which is slower.  window: positions that a token sees, its own among them (0: all).  Both are those of `out` where that is given."""
+    largest tree's, as T takes many small trees for a few large ones, which is slower.  window: positions that a token sees, its own
+    among them (0: all).  Both are those of `out` where that is given."""
     if out is None:
         out = Tree.empty(step.max_tokens, min(max(step.max_tokens, 1), MAX_NODES) if max_nodes is None else max_nodes, window or 0,
                          step.table.device)
@@ -357,8 +358,8 @@ def keep(caches: Sequence["KvCache"], step: Step, tree: Tree, drafted: torch.Ten
          free_state: torch.Tensor, out: Optional[Kept] = None) -> Kept:
     """What stays of a step's drafted tokens (`ivfpq_kv_keep`): of every request its first new token and the longest path behind
     it whose tokens are those that the model picked.  (With masks of the caller's own: the deepest token that sees only tokens that agree, and
-    what it sees; none of a request's where there is no such token, as in a block that sees all of itself and is refused.)  They move together in all caches (of one shape), the boxes of their
-    pages are made again, pages behind them go back to the ring.  tree: the step's, without a window; drafted, picked [T] int32: the
+    what it sees; none of a request's where there is no such token, as in a block that sees all of itself and is refused.)  They move
+    together in all caches (of one shape), the boxes of their pages are made again, pages behind them go back to the ring.  tree: the step's, without a window; drafted, picked [T] int32: the
     tokens, and what the model picks behind each; free_state: `step.free_state`.  Once per step."""
     caches = list(caches)
     _fits(step, tree)
