@@ -359,8 +359,9 @@ def keep(caches: Sequence["KvCache"], step: Step, tree: Tree, drafted: torch.Ten
     """What stays of a step's drafted tokens (`ivfpq_kv_keep`): of every request its first new token and the longest path behind
     it whose tokens are those that the model picked.  (With masks of the caller's own: the deepest token that sees only tokens that agree, and
     what it sees; none of a request's where there is no such token, as in a block that sees all of itself and is refused.)  They move
-    together in all caches (of one shape), the boxes of their pages are made again, pages behind them go back to the ring.  tree: the step's, without a window; drafted, picked [T] int32: the
-    tokens, and what the model picks behind each; free_state: `step.free_state`.  Once per step."""
+    together in all caches (of one shape), the boxes of their pages are made again, pages behind them go back to the ring.  tree: the
+    step's, without a window; drafted, picked [T] int32: the tokens, and what the model picks behind each; free_state:
+    `step.free_state`.  Once per step."""
     caches = list(caches)
     _fits(step, tree)
     dev, T = step._checked, step.max_tokens
